@@ -298,6 +298,76 @@ aa_status agent_attn_fwd_timed(const aa_desc *desc, const void *Q, const void *K
  * descriptor or a NULL / zero-length buffer. */
 size_t agent_attn_plan_str(const aa_desc *desc, int agents_given, char *buf, size_t buf_len);
 
+/* ------------------------------------------------------------------------
+ * Operators of a transformer block around the attention: rotary positions, norms of queries and keys, the gated
+ * feed-forward block.  Conventions as above: device pointers (where not marked as host memory), host-only
+ * validation before anything is launched, no allocation, no synchronisation, the same bits from the same inputs.
+ * ---------------------------------------------------------------------- */
+
+/* A token tensor [batch][heads][tokens][d] in memory: element (b,h,t,c) at b*stride_b + h*stride_h + t*stride_n + c.
+ * All strides 0: dense.  Inputs may repeat an axis (stride 0, not all three); elements of a result must not alias. */
+typedef struct {
+  void *data;
+  int64_t stride_b, stride_h, stride_n;
+} aa_view;
+
+/* Which two channels a pair is, with P = sum of pairs[], S_a = sum of pairs[] before axis a:
+ *   AA_ROPE_ADJACENT     pair j: channels 2j and 2j+1
+ *   AA_ROPE_HALVES       pair j: channels j and P+j
+ *   AA_ROPE_AXIS_HALVES  pair j of axis a (j < pairs[a]): channels 2 S_a + j and 2 S_a + pairs[a] + j */
+typedef enum { AA_ROPE_ADJACENT = 0, AA_ROPE_HALVES = 1, AA_ROPE_AXIS_HALVES = 2 } aa_rope_pairing;
+
+/* Queries and keys and how their channels turn with the position (host memory).  Pair j (all axes' pairs counted
+ * through) of a token at position p along the pair's axis turns by phi = p * freq[j] radians:
+ *   (x, y) -> (x cos phi - y sin phi, x sin phi + y cos phi)
+ * Channels from 2P on pass through.  Angles are formed in 64 bits, so that far positions keep their phase; sines,
+ * cosines and the rotation are in fp32, the result is rounded once to dtype.  d <= 256. */
+typedef struct {
+  int32_t batch, tokens;
+  int32_t heads_q, heads_k; /* heads of the queries and of the keys (shared keys: fewer; 0: queries alone) */
+  int32_t d, dtype;         /* channels of a head; aa_dtype of every token tensor */
+  int32_t pairing;          /* aa_rope_pairing */
+  int32_t axes;             /* 1 .. 4 axes (time, height, width, ...); 0: nothing turns (norms alone) */
+  int32_t pairs[4];         /* pairs of channels that turn by each axis, > 0; 2P <= d */
+  int32_t grid[4];          /* positions are the row-major coordinates of token t on this grid, whose product is
+                               `tokens`; all 0: `positions` are given */
+  const double *freq;       /* HOST memory, [P]: radians per unit of position */
+  const void *positions;    /* NULL with a grid; else [batch][tokens][axes] or [tokens][axes], dense */
+  int32_t positions_float;  /* 0: int32, 1: fp32 */
+  int32_t positions_shared; /* 1: [tokens][axes] for every sequence */
+} aa_rotary;
+
+/* Queries and keys rotated.  Each result may be its own input (same pointer and strides); otherwise results overlap
+ * nothing (AA_ERR_ALIAS), where rows that interleave, as the q / k / v slices of a fused projection do, count as
+ * apart.  k and k_out are not read with heads_k == 0.
+ * Errors: AA_ERR_NULL, AA_ERR_SHAPE (sizes, pairs, grid, strides), AA_ERR_DTYPE, AA_ERR_UNSUPPORTED (d > 256, 2^31 tokens). */
+aa_status agent_rope_fwd(const aa_rotary *desc, const aa_view *q, const aa_view *k, const aa_view *q_out,
+                         const aa_view *k_out, void *hip_stream);
+/* The gradient: rotation by the opposite angles of the results' gradients. */
+aa_status agent_rope_bwd(const aa_rotary *desc, const aa_view *dq_out, const aa_view *dk_out, const aa_view *dq,
+                         const aa_view *dk, void *hip_stream);
+
+/* Norm of every query and key row before the rotation, in the same pass over the tensors:
+ *   y = rotate(w x r),  r = (sum over c of x_c^2 / d + eps)^-1/2
+ * w_q, w_k: device, fp32, [d], or [heads][d] with per_head; NULL: ones.  Sums in fp32.  eps >= 0; a row of zeros with eps
+ * 0 has no norm (NaN). */
+typedef struct {
+  const float *w_q, *w_k;
+  int32_t per_head;
+  float eps;
+} aa_qk_norm;
+aa_status agent_qk_norm_fwd(const aa_rotary *desc, const aa_qk_norm *norm, const aa_view *q, const aa_view *k,
+                            const aa_view *q_out, const aa_view *k_out, void *hip_stream);
+/* Gradients, from q, k and the gradients of the results:  z = rotate back(dy), u = w z,
+ *   dx = r u - x r^3 (sum of u x) / d,   dw = sum over the rows of z x r
+ * dw_q, dw_k: device, fp32, shaped like the weights (or like [d] / [heads][d] without weights), NULL: not wanted;
+ * summed in a fixed order.  dq may be q or dq_out (same pointer and strides), dk likewise.
+ * workspace: agent_qk_norm_bwd_workspace_bytes() (0 for an invalid descriptor), 256-byte aligned; needed for dw_q, dw_k alone. */
+size_t agent_qk_norm_bwd_workspace_bytes(const aa_rotary *desc, const aa_qk_norm *norm);
+aa_status agent_qk_norm_bwd(const aa_rotary *desc, const aa_qk_norm *norm, const aa_view *q, const aa_view *k,
+                            const aa_view *dq_out, const aa_view *dk_out, void *workspace, size_t workspace_bytes,
+                            const aa_view *dq, const aa_view *dk, float *dw_q, float *dw_k, void *hip_stream);
+
 /* Static string for a status code. */
 const char *agent_attn_status_str(int status);
 

@@ -55,12 +55,31 @@ class aa_param_grads(ctypes.Structure):
                 ("ddwc_w", ctypes.c_void_p), ("ddwc_b", ctypes.c_void_p)]
 
 
+class aa_view(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride_b", ctypes.c_int64), ("stride_h", ctypes.c_int64),
+                ("stride_n", ctypes.c_int64)]
+
+
+class aa_rotary(ctypes.Structure):
+    _fields_ = [("batch", ctypes.c_int32), ("tokens", ctypes.c_int32), ("heads_q", ctypes.c_int32),
+                ("heads_k", ctypes.c_int32), ("d", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("pairing", ctypes.c_int32), ("axes", ctypes.c_int32), ("pairs", ctypes.c_int32 * 4),
+                ("grid", ctypes.c_int32 * 4), ("freq", ctypes.c_void_p), ("positions", ctypes.c_void_p),
+                ("positions_float", ctypes.c_int32), ("positions_shared", ctypes.c_int32)]
+
+
+class aa_qk_norm(ctypes.Structure):
+    _fields_ = [("w_q", ctypes.c_void_p), ("w_k", ctypes.c_void_p), ("per_head", ctypes.c_int32),
+                ("eps", ctypes.c_float)]
+
+
 EXPORTS = ("agent_attn_workspace_bytes", "agent_attn_fwd", "agent_pool_fwd", "agent_aggregate_fwd",
            "agent_broadcast_fwd", "agent_attn_flops", "agent_attn_status_str", "agent_attn_plan_str",
            "agent_attn_bwd_workspace_bytes", "agent_attn_bwd", "agent_attn_bias_tables_bytes",
            "agent_attn_bias_tables", "agent_attn_fwd_static", "agent_attn_static_scratch_bytes",
            "agent_attn_fwd_timed", "agent_attn_resize_bias", "agent_attn_module_workspace_bytes",
-           "agent_attn_module_fwd")
+           "agent_attn_module_fwd", "agent_rope_fwd", "agent_rope_bwd", "agent_qk_norm_fwd", "agent_qk_norm_bwd",
+           "agent_qk_norm_bwd_workspace_bytes")
 
 _lib = None
 
@@ -120,6 +139,16 @@ def lib():
         L.agent_attn_bias_tables.argtypes = [dp, pp, vp, ctypes.c_size_t, vp]
         L.agent_attn_plan_str.restype = ctypes.c_size_t
         L.agent_attn_plan_str.argtypes = [dp, ctypes.c_int, ctypes.c_char_p, ctypes.c_size_t]
+        rp, np_, tv = ctypes.POINTER(aa_rotary), ctypes.POINTER(aa_qk_norm), ctypes.POINTER(aa_view)
+        for fn in (L.agent_rope_fwd, L.agent_rope_bwd):
+            fn.restype = ctypes.c_int
+            fn.argtypes = [rp, tv, tv, tv, tv, vp]
+        L.agent_qk_norm_fwd.restype = ctypes.c_int
+        L.agent_qk_norm_fwd.argtypes = [rp, np_, tv, tv, tv, tv, vp]
+        L.agent_qk_norm_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.agent_qk_norm_bwd_workspace_bytes.argtypes = [rp, np_]
+        L.agent_qk_norm_bwd.restype = ctypes.c_int
+        L.agent_qk_norm_bwd.argtypes = [rp, np_, tv, tv, tv, tv, vp, ctypes.c_size_t, tv, tv, vp, vp, vp]
         L.agent_attn_status_str.restype = ctypes.c_char_p
         L.agent_attn_status_str.argtypes = [ctypes.c_int]
         _lib = L
@@ -536,3 +565,194 @@ def agent_broadcast_fwd(Q, A, VA, V=None, *, grid=None, params: dict | None = No
                                    out.data_ptr(), _stream(stream))
     _check(st, "agent_broadcast_fwd")
     return out
+
+
+# --- rotary positions, norms of queries and keys ---
+
+ROPE_PAIRINGS = {"adjacent": 0, "halves": 1, "axis_halves": 2}
+
+
+def rope_frequencies(pairs, base=10000.0, shared=False):
+    """Radians per unit of position of every pair, axis after axis: base^(-j / pairs of the axis) for pair j of its axis,
+    or, shared, base^(-j / P) for pair j of all P (the axes take different parts of one series)."""
+    if shared:
+        total = sum(pairs)
+        return [float(base) ** (-j / total) for j in range(total)]
+    return [float(base) ** (-j / p) for p in pairs for j in range(p)]
+
+
+class Rope:
+    """How the channels of queries and keys turn with the position.
+
+    pairs: pairs of channels turned by each of one to four axes (time, height, width, ...); channels behind them pass.
+    grid: the tokens' grid, one side per axis, row-major; or positions: a dense int32 or float32 device tensor
+    [tokens, axes] or [batch, tokens, axes].  pairing: "adjacent" (2j, 2j+1), "halves" (j, P+j) or "axis_halves" (j and
+    pairs[a]+j within the axis' channels).  freqs: radians per unit of position of every pair (default:
+    rope_frequencies(pairs, base, shared)).  Holds no device memory of its own; one object serves any number of calls."""
+
+    def __init__(self, pairs, *, grid=None, positions=None, pairing="halves", base=10000.0, shared=False, freqs=None):
+        import torch
+        self.pairs = tuple(int(p) for p in pairs)
+        assert 1 <= len(self.pairs) <= 4 and all(p > 0 for p in self.pairs), "one to four axes of at least one pair"
+        assert pairing in ROPE_PAIRINGS, "pairing is one of %s" % (tuple(ROPE_PAIRINGS),)
+        assert (grid is None) != (positions is None), "either a grid or positions"
+        freqs = rope_frequencies(self.pairs, base, shared) if freqs is None else [float(f) for f in freqs]
+        assert len(freqs) == sum(self.pairs), "one frequency for each pair"
+        self._freqs = (ctypes.c_double * len(freqs))(*freqs)
+        self.positions = positions
+        d = aa_rotary(pairing=ROPE_PAIRINGS[pairing], axes=len(self.pairs), freq=ctypes.addressof(self._freqs))
+        d.pairs[:len(self.pairs)] = self.pairs
+        if grid is not None:
+            assert len(grid) == len(self.pairs), "one side of the grid for each axis"
+            d.grid[:len(grid)] = [int(g) for g in grid]
+        else:
+            assert positions.is_cuda and positions.is_contiguous() and positions.dtype in (torch.int32, torch.float32) and \
+                positions.dim() in (2, 3) and positions.shape[-1] == len(self.pairs), \
+                "positions: dense int32 or float32 device tensor [tokens, axes] or [batch, tokens, axes]"
+            d.positions, d.positions_float = positions.data_ptr(), int(positions.dtype == torch.float32)
+            d.positions_shared = int(positions.dim() == 2)
+        self._desc = d
+
+    def _desc_for(self, Q):
+        p = self.positions
+        assert p is None or (p.device == Q.device and p.shape[-2] == Q.shape[2] and
+                             (p.dim() == 2 or p.shape[0] == Q.shape[0])), "positions must match the tokens' batch, number and device"
+        return aa_rotary.from_buffer_copy(self._desc)
+
+
+def _view(t):
+    st = (0, 0, 0) if t.is_contiguous() else (t.stride(0), t.stride(1), t.stride(2))
+    assert t.is_contiguous() or any(st) or t.numel() == t.shape[3], "a tensor repeated along every axis has no view: make it dense"
+    return aa_view(t.data_ptr(), *st)
+
+
+def _check_tokens(what, t, like, heads=None):
+    assert t.is_cuda and t.dim() == 4 and t.dtype == like.dtype and t.device == like.device and \
+        (t.stride(3) == 1 or t.shape[3] == 1), what + " must be [B,H,N,d] on one device, in one dtype, channels side by side"
+    assert t.shape[0] == like.shape[0] and t.shape[2:] == like.shape[2:] and (heads is None or t.shape[1] == heads), \
+        what + " has another batch, number of heads, number of tokens or width"
+
+
+def _rotary_call(Q, K, rope, inputs=(), outputs=None, stream=None):
+    """Descriptor and views of a call: (Q, K), further pairs of `inputs`, and the outputs (fresh where None)."""
+    import torch
+    _check_tokens("Q", Q, Q)
+    if K is not None:
+        _check_tokens("K", K, Q)
+    desc = rope._desc_for(Q) if rope is not None else aa_rotary()
+    desc.batch, desc.heads_q, desc.tokens, desc.d = Q.shape
+    desc.heads_k = K.shape[1] if K is not None else 0
+    desc.dtype = _dtype_code(Q)
+    if outputs is None:
+        outputs = _outputs_like((Q, K), stream)
+    outputs = tuple(outputs)
+    assert len(outputs) == 2 and (outputs[1] is None) == (K is None), "results for Q and, where there is one, for K"
+    for pair in tuple(inputs) + (outputs,):
+        for name, t, like in (("the tensor beside Q", pair[0], Q), ("the tensor beside K", pair[1], K)):
+            if like is None:
+                assert t is None, "no K, so no tensor beside it"
+            else:
+                _check_tokens(name, t, like, like.shape[1])
+    views = [tuple(None if t is None else _view(t) for t in pair) for pair in ((Q, K),) + tuple(inputs) + (outputs,)]
+    return desc, views, outputs
+
+
+def _outputs_like(tensors, stream):
+    """Fresh results in the inputs' order of axes, of the stream that the kernels run on."""
+    import torch
+    if stream is None:
+        return tuple(None if t is None else torch.empty_like(t) for t in tensors)
+    with torch.cuda.stream(stream):
+        return tuple(None if t is None else torch.empty_like(t) for t in tensors)
+
+
+def _ref(v):
+    return None if v is None else ctypes.byref(v)
+
+
+def _check_weights(weights, Q, K):
+    """(w_q, w_k) or None -> aa_qk_norm fields; fp32 [d], or both [heads, d]."""
+    import torch
+    wq, wk = weights if weights is not None else (None, None)
+    per_head = None
+    for w, t, name in ((wq, Q, "w_q"), (wk, K, "w_k")):
+        if w is None:
+            continue
+        assert t is not None and w.is_cuda and w.device == Q.device and w.dtype == torch.float32 and w.is_contiguous(), \
+            name + " must be a dense fp32 tensor on Q's device"
+        assert tuple(w.shape) in ((Q.shape[3],), (t.shape[1], Q.shape[3])), name + " must be [d] or [heads, d]"
+        assert per_head in (None, w.dim() == 2), "w_q and w_k: both [d] or both [heads, d]"
+        per_head = w.dim() == 2
+    return wq, wk, bool(per_head)
+
+
+def _rope_args(Q, K, rope, out, stream):
+    desc, views, outs = _rotary_call(Q, K, rope, (), out, stream)
+    (q, k), (qo, ko) = views
+    return (ctypes.byref(desc), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream(stream)), outs, (desc, views)
+
+
+def agent_rope_fwd(Q, K, rope, *, out=None, stream=None):
+    """Queries Q [B,H,N,d] and keys K [B,H',N,d] (or None) rotated by their positions; any strides, channels side by side.
+    out: (Q', K'), which may be (Q, K) themselves.  Returns (Q', K')."""
+    args, outs, keep = _rope_args(Q, K, rope, out, stream)
+    _check(lib().agent_rope_fwd(*args), "agent_rope_fwd")
+    return outs
+
+
+def agent_rope_bwd(dQ_out, dK_out, rope, *, out=None, stream=None):
+    """Gradients of agent_rope_fwd for the gradients of its results: (dQ, dK)."""
+    args, outs, keep = _rope_args(dQ_out, dK_out, rope, out, stream)
+    _check(lib().agent_rope_bwd(*args), "agent_rope_bwd")
+    return outs
+
+
+def _qk_norm_args(Q, K, rope, weights, eps, out, stream):
+    desc, views, outs = _rotary_call(Q, K, rope, (), out, stream)
+    wq, wk, per_head = _check_weights(weights, Q, K)
+    norm = aa_qk_norm(_ptr(wq), _ptr(wk), int(per_head), eps)
+    (q, k), (qo, ko) = views
+    return (ctypes.byref(desc), ctypes.byref(norm), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream(stream)), outs, \
+        (desc, norm, views)
+
+
+def agent_qk_norm_fwd(Q, K, rope=None, *, weights=None, eps=1e-6, out=None, stream=None):
+    """Every row of Q and K divided by its root mean square, times its weights, then rotated (rope None: not), in one
+    pass.  weights: (w_q, w_k), fp32, both [d] or both [heads, d]; None: ones.  Tensors as for agent_rope_fwd."""
+    args, outs, keep = _qk_norm_args(Q, K, rope, weights, eps, out, stream)
+    _check(lib().agent_qk_norm_fwd(*args), "agent_qk_norm_fwd")
+    return outs
+
+
+def agent_qk_norm_bwd(Q, K, dQ_out, dK_out, rope=None, *, weights=None, eps=1e-6, want_weight_grads=True, out=None,
+                      workspace=None, stream=None):
+    """Gradients of agent_qk_norm_fwd: a dict of dq, dk (None without K) and, for the weights present and
+    want_weight_grads, dw_q, dw_k (fp32).  out: (dQ, dK), which may be (Q, K) or (dQ_out, dK_out)."""
+    import torch
+    desc, views, outs = _rotary_call(Q, K, rope, ((dQ_out, dK_out),), out, stream)
+    wq, wk, per_head = _check_weights(weights, Q, K)
+    norm = aa_qk_norm(_ptr(wq), _ptr(wk), int(per_head), eps)
+    dw = _outputs_like((wq, wk) if want_weight_grads else (None, None), stream)
+    need = 0
+    if dw != (None, None):
+        need = int(lib().agent_qk_norm_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(norm)))
+        if workspace is None:
+            workspace = _alloc_bytes(max(need, 256), stream, Q.device)
+        assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == Q.device
+    (q, k), (gq, gk), (dq, dk) = views
+    st = lib().agent_qk_norm_bwd(ctypes.byref(desc), ctypes.byref(norm), _ref(q), _ref(k), _ref(gq), _ref(gk), _ptr(workspace),
+                                 0 if workspace is None else workspace.numel() * workspace.element_size(), _ref(dq), _ref(dk),
+                                 _ptr(dw[0]), _ptr(dw[1]), _stream(stream))
+    _check(st, "agent_qk_norm_bwd")
+    grads = {"dq": outs[0], "dk": outs[1], "dw_q": dw[0], "dw_k": dw[1]}
+    return {name: t for name, t in grads.items() if t is not None}
+
+
+def prepare_rope(Q, K, rope, *, out, stream=None) -> PreparedCall:
+    args, outs, keep = _rope_args(Q, K, rope, out, stream)
+    return PreparedCall(lib().agent_rope_fwd, "agent_rope_fwd", args, (keep, Q, K, rope, outs))
+
+
+def prepare_qk_norm(Q, K, rope=None, *, weights=None, eps=1e-6, out, stream=None) -> PreparedCall:
+    args, outs, keep = _qk_norm_args(Q, K, rope, weights, eps, out, stream)
+    return PreparedCall(lib().agent_qk_norm_fwd, "agent_qk_norm_fwd", args, (keep, Q, K, rope, weights, outs))

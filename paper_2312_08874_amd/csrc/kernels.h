@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "rotary.h"
 
 namespace aa {
 
@@ -122,6 +123,15 @@ bool forward_f32_supported(const Problem& p);
 size_t forward_f32_workspace_floats(const Problem& p);
 hipError_t launch_forward_f32(const Problem& p, const void* Q, const void* K, const void* V, const void* A, float* ws,
                               void* out, hipStream_t st);
+
+// --- rotary positions, norms of queries and keys: rotary.hip, and one unit per element type ---
+hipError_t launch_rotary_f32(const RotaryArgs& a, const RotaryShape& s, RotaryMode mode, int chunk, int blocks, hipStream_t st);
+hipError_t launch_rotary_f16(const RotaryArgs& a, const RotaryShape& s, RotaryMode mode, int chunk, int blocks, hipStream_t st);
+hipError_t launch_rotary_bf16(const RotaryArgs& a, const RotaryShape& s, RotaryMode mode, int chunk, int blocks, hipStream_t st);
+// fp32 scratch of the backward pass (a.partial)
+size_t rotary_partial_floats(const RotaryArgs& a);
+// dw_q, dw_k: gradients of the norm's weights, backward pass alone, null where they are not wanted
+hipError_t launch_rotary(int dtype, RotaryArgs& a, const RotaryShape& s, RotaryMode mode, float* dw_q, float* dw_k, hipStream_t st);
 
 // --- small-agent regime (n <= 64, d in {32, 64}, fp16 / bf16): MFMA kernels that keep A and V_A in
 //     registers and stream tokens straight from global memory ---
