@@ -368,6 +368,49 @@ aa_status agent_qk_norm_bwd(const aa_rotary *desc, const aa_qk_norm *norm, const
                             const aa_view *dq_out, const aa_view *dk_out, void *workspace, size_t workspace_bytes,
                             const aa_view *dq, const aa_view *dk, float *dw_q, float *dw_k, void *hip_stream);
 
+/* The gated feed-forward block of `rows` tokens (host struct; sizes in elements):
+ *   gate = x Wg^T + bg,  up = x Wu^T + bu,  h = act(gate) * up,  y = h Wd^T + bd
+ * x, y [rows][width]; Wg, Wu [hidden][width], Wd [width][hidden], all row-major and dense, biases [hidden], [hidden],
+ * [width] or NULL; everything in `dtype`.  Sums are fp32; h is rounded to dtype between the products, results are
+ * rounded once.  Rows of x, y, dy and dx may be apart (strides in elements, 0: dense).  Tensors of any alignment
+ * and width are taken; those whose rows are no whole 16-byte pieces are copied to the workspace first.
+ * width, hidden <= 2^20, rows * max(width, hidden) < 2^40. */
+typedef enum { AA_SILU = 0, AA_GELU = 1, AA_GELU_TANH = 2, AA_RELU = 3, AA_SIGMOID = 4 } aa_activation;
+typedef struct {
+  int32_t rows, width, hidden;
+  int32_t dtype;            /* aa_dtype */
+  int32_t activation;       /* aa_activation; AA_GELU is g * Phi(g), AA_GELU_TANH its approximation by tanh */
+  int64_t x_stride, y_stride, dx_stride; /* of the rows of x; of y and dy; of dx */
+} aa_ffn;
+typedef struct {
+  const void *w_gate, *b_gate; /* [hidden][width], [hidden] or NULL */
+  const void *w_up, *b_up;
+  const void *w_down, *b_down; /* [width][hidden], [width] or NULL */
+} aa_ffn_weights;
+/* Device gradients of the weights, shaped and typed like them; NULL: not wanted (a bias may be asked for that was NULL). */
+typedef struct {
+  void *dw_gate, *db_gate, *dw_up, *db_up, *dw_down, *db_down;
+} aa_ffn_grads;
+
+/* Bytes of device workspace of either pass, and of what the forward pass keeps for the backward pass (h, and the
+ * derivatives of h by gate and by up: 8 bytes a hidden channel of a token for 16-bit types, 12 for fp32).  0 for an
+ * invalid descriptor. */
+size_t agent_gated_ffn_workspace_bytes(const aa_ffn *desc);
+size_t agent_gated_ffn_saved_bytes(const aa_ffn *desc);
+size_t agent_gated_ffn_bwd_workspace_bytes(const aa_ffn *desc);
+
+/* Forward pass.  saved: NULL, or agent_gated_ffn_saved_bytes() of device memory that the backward pass of these rows
+ * reads; saved and workspace 256-byte aligned (AA_ERR_WORKSPACE).  y overlaps nothing. */
+aa_status agent_gated_ffn_fwd(const aa_ffn *desc, const void *x, const aa_ffn_weights *weights, void *saved,
+                              void *workspace, size_t workspace_bytes, void *y, void *hip_stream);
+/* Backward pass for the gradient dy of y; x and the weights as in the forward pass (the biases are not read):
+ *   dh = dy Wd;  dgate = dh * up * act'(gate), dup = dh * act(gate);  dx = dgate Wg + dup Wu;
+ *   dWg = dgate^T x, dWu = dup^T x, dWd = dy^T h; biases: sums over the rows of dgate, dup, dy.
+ * dgate and dup are rounded to dtype, as operands of the products.  dx NULL: not wanted.  Results overlap nothing. */
+aa_status agent_gated_ffn_bwd(const aa_ffn *desc, const void *x, const aa_ffn_weights *weights, const void *saved,
+                              const void *dy, void *workspace, size_t workspace_bytes, void *dx,
+                              const aa_ffn_grads *grads, void *hip_stream);
+
 /* Static string for a status code. */
 const char *agent_attn_status_str(int status);
 

@@ -73,13 +73,28 @@ class aa_qk_norm(ctypes.Structure):
                 ("eps", ctypes.c_float)]
 
 
+class aa_ffn(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("hidden", ctypes.c_int32),
+                ("dtype", ctypes.c_int32), ("activation", ctypes.c_int32), ("x_stride", ctypes.c_int64),
+                ("y_stride", ctypes.c_int64), ("dx_stride", ctypes.c_int64)]
+
+
+class aa_ffn_weights(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("w_gate", "b_gate", "w_up", "b_up", "w_down", "b_down")]
+
+
+class aa_ffn_grads(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("dw_gate", "db_gate", "dw_up", "db_up", "dw_down", "db_down")]
+
+
 EXPORTS = ("agent_attn_workspace_bytes", "agent_attn_fwd", "agent_pool_fwd", "agent_aggregate_fwd",
            "agent_broadcast_fwd", "agent_attn_flops", "agent_attn_status_str", "agent_attn_plan_str",
            "agent_attn_bwd_workspace_bytes", "agent_attn_bwd", "agent_attn_bias_tables_bytes",
            "agent_attn_bias_tables", "agent_attn_fwd_static", "agent_attn_static_scratch_bytes",
            "agent_attn_fwd_timed", "agent_attn_resize_bias", "agent_attn_module_workspace_bytes",
            "agent_attn_module_fwd", "agent_rope_fwd", "agent_rope_bwd", "agent_qk_norm_fwd", "agent_qk_norm_bwd",
-           "agent_qk_norm_bwd_workspace_bytes")
+           "agent_qk_norm_bwd_workspace_bytes", "agent_gated_ffn_workspace_bytes", "agent_gated_ffn_saved_bytes",
+           "agent_gated_ffn_bwd_workspace_bytes", "agent_gated_ffn_fwd", "agent_gated_ffn_bwd")
 
 _lib = None
 
@@ -149,6 +164,14 @@ def lib():
         L.agent_qk_norm_bwd_workspace_bytes.argtypes = [rp, np_]
         L.agent_qk_norm_bwd.restype = ctypes.c_int
         L.agent_qk_norm_bwd.argtypes = [rp, np_, tv, tv, tv, tv, vp, ctypes.c_size_t, tv, tv, vp, vp, vp]
+        fp, wp, gp = ctypes.POINTER(aa_ffn), ctypes.POINTER(aa_ffn_weights), ctypes.POINTER(aa_ffn_grads)
+        for fn in (L.agent_gated_ffn_workspace_bytes, L.agent_gated_ffn_saved_bytes, L.agent_gated_ffn_bwd_workspace_bytes):
+            fn.restype = ctypes.c_size_t
+            fn.argtypes = [fp]
+        L.agent_gated_ffn_fwd.restype = ctypes.c_int
+        L.agent_gated_ffn_fwd.argtypes = [fp, vp, wp, vp, vp, ctypes.c_size_t, vp, vp]
+        L.agent_gated_ffn_bwd.restype = ctypes.c_int
+        L.agent_gated_ffn_bwd.argtypes = [fp, vp, wp, vp, vp, vp, ctypes.c_size_t, vp, gp, vp]
         L.agent_attn_status_str.restype = ctypes.c_char_p
         L.agent_attn_status_str.argtypes = [ctypes.c_int]
         _lib = L
@@ -756,3 +779,103 @@ def prepare_rope(Q, K, rope, *, out, stream=None) -> PreparedCall:
 def prepare_qk_norm(Q, K, rope=None, *, weights=None, eps=1e-6, out, stream=None) -> PreparedCall:
     args, outs, keep = _qk_norm_args(Q, K, rope, weights, eps, out, stream)
     return PreparedCall(lib().agent_qk_norm_fwd, "agent_qk_norm_fwd", args, (keep, Q, K, rope, weights, outs))
+
+
+# --- the gated feed-forward block ---
+
+ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
+
+
+def _ffn_rows(what, t, like):
+    """A [..., width] tensor whose rows lie one stride apart: that stride (0: dense)."""
+    assert t.is_cuda and t.device == like.device and t.dtype == like.dtype and tuple(t.shape) == tuple(like.shape), \
+        what + " must have x's shape, dtype and device"
+    if t.is_contiguous():
+        return 0
+    assert t.dim() == 2 and (t.stride(1) == 1 or t.shape[1] == 1) and (t.stride(0) >= t.shape[1] or t.shape[0] == 1), \
+        what + ": rows one stride apart, [rows, width], or dense"
+    return t.stride(0) if t.shape[0] > 1 else 0
+
+
+def _ffn_call(x, w_gate, w_up, w_down, b_gate, b_up, b_down, activation):
+    assert x.is_cuda and x.dim() >= 2 and x.numel() > 0, "x is a device tensor [..., width]"
+    C, F = x.shape[-1], w_gate.shape[0]
+    for t, shape, name in ((w_gate, (F, C), "w_gate"), (w_up, (F, C), "w_up"), (w_down, (C, F), "w_down"),
+                           (b_gate, (F,), "b_gate"), (b_up, (F,), "b_up"), (b_down, (C,), "b_down")):
+        assert t is None or (t.is_cuda and t.device == x.device and t.dtype == x.dtype and t.is_contiguous() and
+                             tuple(t.shape) == shape), name + " must be a dense tensor of x's dtype and device, shaped %s" % (shape,)
+    assert w_gate is not None and w_up is not None and w_down is not None
+    assert activation in ACTIVATIONS, "activation is one of %s" % (tuple(ACTIVATIONS),)
+    desc = aa_ffn(x.numel() // C, C, F, _dtype_code(x), ACTIVATIONS[activation], _ffn_rows("x", x, x), 0, 0)
+    w = aa_ffn_weights(w_gate.data_ptr(), _ptr(b_gate), w_up.data_ptr(), _ptr(b_up), w_down.data_ptr(), _ptr(b_down))
+    return desc, w
+
+
+def _ffn_workspace(need, workspace, stream, device):
+    if workspace is None:
+        return _alloc_bytes(max(need, 256), stream, device)
+    assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == device
+    return workspace
+
+
+def _ffn_fwd_args(x, w, desc, out, saved, workspace, stream):
+    desc.y_stride = _ffn_rows("out", out, x)
+    workspace = _ffn_workspace(int(lib().agent_gated_ffn_workspace_bytes(ctypes.byref(desc))), workspace, stream, x.device)
+    return (ctypes.byref(desc), x.data_ptr(), ctypes.byref(w), _ptr(saved), workspace.data_ptr(),
+            workspace.numel() * workspace.element_size(), out.data_ptr(), _stream(stream)), workspace
+
+
+def agent_gated_ffn_fwd(x, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu", save=False,
+                        out=None, workspace=None, stream=None):
+    """y = (act(x w_gate^T + b_gate) * (x w_up^T + b_up)) w_down^T + b_down for x [..., width], weights [hidden, width],
+    [hidden, width], [width, hidden] and biases in x's dtype.  activation: "silu", "gelu", "gelu_tanh", "relu" or "sigmoid".
+    save: also returns what agent_gated_ffn_bwd needs, (y, saved)."""
+    desc, w = _ffn_call(x, w_gate, w_up, w_down, b_gate, b_up, b_down, activation)
+    if out is None:
+        out = _dense_like(x, stream)
+    saved = _alloc_bytes(int(lib().agent_gated_ffn_saved_bytes(ctypes.byref(desc))), stream, x.device) if save else None
+    args, keep = _ffn_fwd_args(x, w, desc, out, saved, workspace, stream)
+    _check(lib().agent_gated_ffn_fwd(*args), "agent_gated_ffn_fwd")
+    return (out, saved) if save else out
+
+
+def _dense_like(t, stream):
+    import torch
+    if stream is None:
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+    with torch.cuda.stream(stream):
+        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+
+
+def agent_gated_ffn_bwd(x, dy, saved, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu",
+                        want_dx=True, want_weight_grads=True, workspace=None, stream=None):
+    """Gradients of agent_gated_ffn_fwd for the gradient dy of its result; saved: what that call returned.  A dict of dx
+    (want_dx) and, with want_weight_grads, dw_gate, dw_up, dw_down and db_* for the biases present, in x's dtype."""
+    import torch
+    desc, w = _ffn_call(x, w_gate, w_up, w_down, b_gate, b_up, b_down, activation)
+    desc.y_stride = _ffn_rows("dy", dy, x)
+    assert saved.is_cuda and saved.device == x.device and saved.dtype == torch.uint8 and saved.is_contiguous() and \
+        saved.numel() >= int(lib().agent_gated_ffn_saved_bytes(ctypes.byref(desc))), "saved is what the forward pass returned"
+    out, g = {}, aa_ffn_grads()
+    if want_dx:
+        out["dx"] = _dense_like(x, stream)
+    if want_weight_grads:
+        for name, t in (("w_gate", w_gate), ("w_up", w_up), ("w_down", w_down), ("b_gate", b_gate), ("b_up", b_up),
+                        ("b_down", b_down)):
+            if t is not None:
+                out["d" + name] = _dense_like(t, stream)
+                setattr(g, "d" + name, out["d" + name].data_ptr())
+    workspace = _ffn_workspace(int(lib().agent_gated_ffn_bwd_workspace_bytes(ctypes.byref(desc))), workspace, stream, x.device)
+    st = lib().agent_gated_ffn_bwd(ctypes.byref(desc), x.data_ptr(), ctypes.byref(w), saved.data_ptr(), dy.data_ptr(),
+                                   workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(out.get("dx")),
+                                   ctypes.byref(g), _stream(stream))
+    _check(st, "agent_gated_ffn_bwd")
+    return out
+
+
+def prepare_gated_ffn(x, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu", out,
+                      workspace=None, stream=None) -> PreparedCall:
+    desc, w = _ffn_call(x, w_gate, w_up, w_down, b_gate, b_up, b_down, activation)
+    args, workspace = _ffn_fwd_args(x, w, desc, out, None, workspace, stream)
+    return PreparedCall(lib().agent_gated_ffn_fwd, "agent_gated_ffn_fwd", args,
+                        (desc, w, x, w_gate, w_up, w_down, b_gate, b_up, b_down, workspace, out))

@@ -1,0 +1,9 @@
+#include "kernels.h"
+
+#include "ffn_kernels.inc"
+
+namespace aa {
+hipError_t launch_ffn_product_bf16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st) {
+  return product<ElemBF16>(a, form, epi, t, st);
+}
+}  // namespace aa

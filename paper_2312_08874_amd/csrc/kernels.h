@@ -5,6 +5,7 @@
 #include <stdint.h>
 
 #include "common.h"
+#include "ffn.h"
 #include "rotary.h"
 
 namespace aa {
@@ -132,6 +133,16 @@ hipError_t launch_rotary_bf16(const RotaryArgs& a, const RotaryShape& s, RotaryM
 size_t rotary_partial_floats(const RotaryArgs& a);
 // dw_q, dw_k: gradients of the norm's weights, backward pass alone, null where they are not wanted
 hipError_t launch_rotary(int dtype, RotaryArgs& a, const RotaryShape& s, RotaryMode mode, float* dw_q, float* dw_k, hipStream_t st);
+
+// --- the gated feed-forward block: ffn.hip, and one unit per element type ---
+hipError_t launch_ffn_product_f32(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
+hipError_t launch_ffn_product_f16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
+hipError_t launch_ffn_product_bf16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
+size_t ffn_saved_bytes(const FfnBlock& b);
+size_t ffn_fwd_workspace(const FfnBlock& b);
+size_t ffn_bwd_workspace(const FfnBlock& b);
+hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* ws, hipStream_t st);
+hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* ws, hipStream_t st);
 
 // --- small-agent regime (n <= 64, d in {32, 64}, fp16 / bf16): MFMA kernels that keep A and V_A in
 //     registers and stream tokens straight from global memory ---
