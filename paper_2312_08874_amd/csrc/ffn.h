@@ -48,6 +48,19 @@ struct FfnProduct {
   uint8_t *p_lo, *q_lo;
 };
 
+// A few tokens: x -> h (w: gate and up, K = width, N = hidden) and h -> y (w[0]: down, K = hidden, N = width).  Weights [N][K], dense.
+constexpr int kFfnFewRows = 64;
+struct FfnRows {
+  const void *w[2], *x, *bias[2];
+  long long ldx, ldy;
+  int M, N, K, pitch, activation;      // pitch: of h and of what is kept
+  void *h, *kept_h, *y;                // h: 16 bits (up to four tokens: two terms, [2][M][pitch]) or fp32; kept_h, p and q for the backward pass, where p_hi is set
+  uint16_t *p_hi, *q_hi;
+  uint8_t *p_lo, *q_lo;
+};
+// Waves of a block, which share out the steps of 64 bytes.
+inline int ffn_rows_waves(int steps) { return steps >= 16 ? 8 : 4; }
+
 // which operands are m-contiguous: A and B k-contiguous, B alone m-contiguous, both
 enum class FfnForm { kKK, kKM, kMM };
 

@@ -137,7 +137,7 @@ Plan make_plan(const FfnBlock& b, bool backward) {
   w.w_up = take((size_t)b.F * C * es);
   w.w_down = take((size_t)b.C * F * es);
   if (backward) w.dgu = take((size_t)b.T * 2 * pitch * es);
-  else w.h = take((size_t)b.T * pitch * es);
+  else w.h = take((size_t)b.T * pitch * (b.T <= kFfnFewRows ? 4 : es));
   size_t part = 0;
   if (backward) {
     part = std::max({partial_bytes(p.dx, b.T, b.C), partial_bytes(p.dw_in, 2 * (long long)pitch, b.C), partial_bytes(p.dw_down, b.C, b.F),
@@ -247,9 +247,34 @@ size_t ffn_bwd_workspace(const FfnBlock& b) { return make_plan(b, true).total; }
     if (err_ != hipSuccess) return err_;      \
   } while (0)
 
+namespace {
+
+hipError_t launch_rows(int dtype, const FfnRows& a, bool gate, int es, hipStream_t st) {
+  const int waves = ffn_rows_waves((a.K * es + 63) / 64);
+  if (dtype == 0) return launch_ffn_rows_f32(a, gate, waves, st);
+  return dtype == 1 ? launch_ffn_rows_f16(a, gate, waves, st) : launch_ffn_rows_bf16(a, gate, waves, st);
+}
+
+hipError_t few_rows_fwd(const FfnBlock& b, char* keep, void* h, hipStream_t st) {
+  const Saved s = saved_plan(b);
+  FfnRows a{};
+  a.w[0] = b.w_gate, a.w[1] = b.w_up, a.x = b.x, a.ldx = b.ldx, a.bias[0] = b.b_gate, a.bias[1] = b.b_up;
+  a.M = b.T, a.N = b.F, a.K = b.C, a.pitch = ffn_pitch(b.F), a.activation = b.activation, a.h = h;
+  if (keep) {
+    a.kept_h = keep + s.h, a.p_hi = (uint16_t*)(keep + s.p_hi), a.q_hi = (uint16_t*)(keep + s.q_hi);
+    a.p_lo = (uint8_t*)(keep + s.p_lo), a.q_lo = (uint8_t*)(keep + s.q_lo);
+  }
+  AA_TRY(launch_rows(b.dtype, a, true, b.es(), st));
+  a.w[0] = b.w_down, a.bias[0] = b.b_down, a.N = b.C, a.K = b.F, a.y = b.y, a.ldy = b.ldy;
+  return launch_rows(b.dtype, a, false, b.es(), st);
+}
+
+}  // namespace
+
 hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* workspace, hipStream_t st) {
   char* ws = (char*)workspace;
   const Plan w = make_plan(b, false);
+  if (b.T <= kFfnFewRows) return few_rows_fwd(b, (char*)saved, ws + w.h, st);
   const Products p = products(b);
   const Saved s = saved_plan(b);
   const int pitch = ffn_pitch(b.F), unit = b.unit();

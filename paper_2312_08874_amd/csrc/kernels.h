@@ -138,6 +138,9 @@ hipError_t launch_rotary(int dtype, RotaryArgs& a, const RotaryShape& s, RotaryM
 hipError_t launch_ffn_product_f32(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
 hipError_t launch_ffn_product_f16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
 hipError_t launch_ffn_product_bf16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
+hipError_t launch_ffn_rows_f32(const FfnRows& a, bool gate, int waves, hipStream_t st);
+hipError_t launch_ffn_rows_f16(const FfnRows& a, bool gate, int waves, hipStream_t st);
+hipError_t launch_ffn_rows_bf16(const FfnRows& a, bool gate, int waves, hipStream_t st);
 size_t ffn_saved_bytes(const FfnBlock& b);
 size_t ffn_fwd_workspace(const FfnBlock& b);
 size_t ffn_bwd_workspace(const FfnBlock& b);
