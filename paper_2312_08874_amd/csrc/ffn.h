@@ -15,7 +15,6 @@ inline int ffn_pitch(int hidden) { return (hidden + kFfnPad - 1) / kFfnPad * kFf
 
 enum class FfnEpilogue {
   kStore,        // out[m][n] = sum (+ bias[n]), rounded to the element type; rows from row_part on go to out[1]
-  kPartial,      // partial[split][m][n] = sum over the split's part of k, fp32
   kGate,         // n is hidden: h = act(gate) up, and what the backward pass needs of it
   kGateGrad,     // n is hidden: sum = dh; dgate = dh p, dup = dh q
 };
@@ -30,7 +29,6 @@ struct FfnProduct {
   int a_m, b_m;          // columns of an m-contiguous operand, whole pieces of 16 bytes
   int k_part, b_rows;    // b_parts == 2: a multiple of kFfnPad; rows of an m-contiguous B (of each part), zeros behind them
   int b_parts;
-  int splits, split_steps;      // k is cut into `splits` of split_steps steps
   int grid_m, grid_n;
   // epilogues
   void* out[2];
@@ -39,14 +37,42 @@ struct FfnProduct {
   int rows;
   int aligned;                  // 16-byte stores may be used
   const void* bias[2];          // kStore: [0]; kGate: gate, up
-  float* partial;
-  int pitch;                    // of h, p, q, dgate | dup (two of them) and of a row of `partial`
+  int pitch;                    // of h, p, q, and (two of them) dgate | dup
   int hidden;                   // kGate, kGateGrad
   int activation;
   void* h;
   uint16_t *p_hi, *q_hi;        // d h / d gate and d h / d up, upper 16 and next 8 bits of fp32 (fp32 elements: all in p_hi)
   uint8_t *p_lo, *q_lo;
 };
+
+// which operands are m-contiguous: A and B k-contiguous, B alone m-contiguous, both
+enum class FfnForm { kKK, kKM, kMM };
+
+// A block's tile; `full` tiles are summed by one block each, the others by `parts` blocks of `each` steps.
+struct FfnTile {
+  int rows, cols, full, parts, each;
+};
+// One or two products of one form over the same k in one launch: tiles from `first` on are the second's.
+struct FfnGroup {
+  FfnProduct p[2];
+  int first, tiles, full, parts, each;
+  float* partial;      // [part][tile - full][rows][cols]
+};
+
+#ifdef __HIPCC__
+#define AA_HOST_DEVICE __host__ __device__ __forceinline__
+#else
+#define AA_HOST_DEVICE inline
+#endif
+// Tile `at` of a grid of tiles: eight rows of tiles down before the next column, so that neighbours share operands.
+AA_HOST_DEVICE void ffn_place(unsigned at, unsigned grid_m, unsigned grid_n, int& tm, int& tn) {
+  const unsigned group = 8u * grid_n, gi = at / group, rest = at - gi * group, left = grid_m - 8u * gi, high = left < 8u ? left : 8u;
+  tm = (int)(8u * gi + rest % high);
+  tn = (int)(rest / high);
+}
+// Block L of `count` (of the grid's rounded up to eights): each of the eight XCDs, to which blocks go in turn, takes a run of
+// neighbours, so that its L2 serves what they share.  count or more: no work.
+AA_HOST_DEVICE unsigned ffn_run(unsigned L, unsigned count) { return (L & 7u) * ((count + 7u) / 8u) + (L >> 3); }
 
 // A few tokens: x -> h (w: gate and up, K = width, N = hidden) and h -> y (w[0]: down, K = hidden, N = width).  Weights [N][K], dense.
 constexpr int kFfnFewRows = 64;
@@ -61,13 +87,6 @@ struct FfnRows {
 // Waves of a block, which share out the steps of 64 bytes.
 inline int ffn_rows_waves(int steps) { return steps >= 16 ? 8 : 4; }
 
-// which operands are m-contiguous: A and B k-contiguous, B alone m-contiguous, both
-enum class FfnForm { kKK, kKM, kMM };
-
-struct FfnTile {
-  int rows, cols, splits;      // of a block; parts that k is cut into
-};
-
 // The block as its caller describes it; rows of `ld` elements where they may be apart.
 struct FfnBlock {
   int T, C, F, dtype, activation;      // tokens, width, hidden width
@@ -80,28 +99,47 @@ struct FfnBlock {
   int unit() const { return 16 / es(); }      // elements of 16 bytes
 };
 
-// Tile and parts of k of a product of M x N results over `steps` steps of 128 bytes: the least estimated time.  A compute unit
-// holds one block of 256 x 256, two of 128 x 128, four of 64 x 64 (which alone has work for few rows).
-inline FfnTile ffn_tile(long long M, long long N, int steps, int es, bool can_split, bool gated, int compute_units) {
+// Tile of one or two products (second: M2 x N2, or 0) over `steps` steps of 128 bytes, and how the tiles that are left after whole
+// rounds of the compute units are shared out along k (`split`: whether they may be): the least estimated time.
+//
+// Microseconds, measured over 4 to 36 steps (16-bit elements, k-contiguous operands; m-contiguous ones within 8 %): a step of as
+// many blocks as a compute unit holds, of one alone, and what a block costs beside its steps.  fp32 steps are those of its matrix
+// rate.
+inline FfnTile ffn_tile(long long M, long long N, long long M2, long long N2, int steps, int es, bool split, bool gated, int compute_units) {
   struct Shape {
-    int size, held;
-    double step, least, fixed;      // microseconds: of a step with a full compute unit, of one block alone, of a block's start and end
+    int rows, cols, held;
+    double step, alone, fixed, fixed_alone;
   };
-  static const Shape shapes[3] = {{256, 1, 2.2, 2.2, 5.0}, {128, 2, 1.5, 0.9, 3.0}, {64, 4, 1.3, 0.7, 2.0}};
-  FfnTile best{64, 64, 1};
+  static const Shape half[4] = {{256, 256, 1, 1.38, 1.38, 9.0, 9.0}, {256, 128, 1, 0.78, 0.78, 5.0, 5.0}, {128, 128, 2, 0.84, 0.56, 6.0, 3.5}, {64, 64, 4, 0.74, 0.35, 3.5, 1.5}};
+  static const Shape single[2] = {{128, 128, 2, 3.75, 2.05, 8.0, 5.0}, {64, 64, 4, 2.0, 0.62, 4.5, 2.0}};
+  FfnTile best{64, 64, 1, 1, steps};
   double least = 1e30;
-  for (const Shape& s : shapes) {
-    if (s.size == 256 && es == 4) continue;
-    const long long cols = gated ? s.size / 2 : s.size, blocks = ((M + s.size - 1) / s.size) * ((N + cols - 1) / cols);
-    for (int splits = 1; splits <= 64; splits *= 2) {
-      if (splits > 1 && (!can_split || steps / splits < 4)) break;
-      const int each = (steps + splits - 1) / splits, parts = (steps + each - 1) / each;
-      const long long total = blocks * parts, room = (long long)compute_units * s.held, rounds = (total + room - 1) / room;
-      const long long on_one = std::min<long long>((total + compute_units - 1) / compute_units, s.held);
-      const double slow = es == 4 ? 8.0 : 1.0, step = std::max(s.least, s.step * slow * on_one / s.held);
-      double t = rounds * (each * step + s.fixed);
-      if (parts > 1) t += 4.0 + 8e-6 * parts * M * N / 4.0;      // written and read again, 4 TB/s
-      if (t < least) least = t, best = FfnTile{s.size, s.size, parts};
+  for (int i = 0; i < (es == 4 ? 2 : 4); ++i) {
+    const Shape& s = es == 4 ? single[i] : half[i];
+    const long long cols = gated ? s.cols / 2 : s.cols;
+    const long long tiles = (M + s.rows - 1) / s.rows * ((N + cols - 1) / cols) + (M2 + s.rows - 1) / s.rows * ((N2 + cols - 1) / cols);
+    const long long room = (long long)compute_units * s.held;
+    // of `blocks` blocks of `each` steps, dealt out evenly
+    auto time = [&](long long blocks, int each) {
+      const long long per = (blocks + compute_units - 1) / compute_units, whole = per / s.held, rest = per % s.held;
+      const double share = s.held > 1 ? (double)(rest - 1) / (s.held - 1) : 0.0;
+      double t = whole * (each * s.step + s.fixed);
+      if (rest > 0) t += each * (s.alone + share * (s.step - s.alone)) + s.fixed_alone + share * (s.fixed - s.fixed_alone);
+      return t;
+    };
+    auto consider = [&](long long full, int parts, int each) {
+      double t = time(full, steps);
+      if (parts > 1)      // their sums are written, read and added up by one more launch
+        t += time((tiles - full) * parts, each) + 4.0 + 8.0e-6 * (tiles - full) * parts * s.rows * s.cols / 4.5;
+      if (t < least) least = t, best = FfnTile{s.rows, s.cols, (int)full, parts, each};
+    };
+    consider(tiles, 1, steps);
+    if (!split) continue;
+    const long long full = tiles / room * room;      // whole rounds
+    if (full == tiles) continue;
+    for (int parts = 2; parts <= 64 && steps / parts >= 2; ++parts) {
+      const int each = (steps + parts - 1) / parts;
+      if ((steps + each - 1) / each == parts) consider(full, parts, each);
     }
   }
   return best;

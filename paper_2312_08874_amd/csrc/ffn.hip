@@ -46,35 +46,40 @@ __global__ __launch_bounds__(256) void ffn_copy_kernel(CopyJobs jobs) {
   }
 }
 
-// out[row][n] = sum over the parts of partial[part][row][n] (+ bias[n]), rounded once; rows from row_part on go to out1, rows of a
-// part past `rows` nowhere.  The parts in their order.
-struct SumArgs {
-  const float* partial;
-  int parts, M, N, pitch, row_part, rows;
-  long long ldo;
-  void *out0, *out1;
-  const void* bias;
-};
+// The tiles of a group that were summed in parts: the parts in their order, the bias, one rounding.  A block takes 1024 results.
 template <class E>
-__global__ __launch_bounds__(256) void ffn_sum_kernel(SumArgs a) {
+__global__ __launch_bounds__(256) void ffn_sum_kernel(FfnGroup g, int rows, int cols) {
   using T = typename E::T;
-  const int quads = (a.N + 3) / 4;
-  const long long at = (long long)blockIdx.x * 256 + threadIdx.x, row = at / quads;
-  const int n = (int)(at - row * quads) * 4;
-  if (row >= a.M) return;
+  const unsigned rest = blockIdx.y, tile = g.full + rest, tail = g.tiles - g.full;
+  const int q = (int)(blockIdx.x * 256 + threadIdx.x) * 4, in = q / cols, c = q - in * cols;
+  FfnProduct a = g.p[0];
+  if (tile >= (unsigned)g.first) a = g.p[1];
+  int tm, tn;
+  ffn_place(tile >= (unsigned)g.first ? tile - g.first : tile, a.grid_m, a.grid_n, tm, tn);
+  const int row = tm * rows + in, n = tn * cols + c;
+  if (row >= a.M || n >= a.N) return;
   const bool second = a.row_part > 0 && row >= a.row_part;
-  const long long rr = second ? row - a.row_part : row;
-  T* to = (T*)(second ? a.out1 : a.out0);
+  const int rr = second ? row - a.row_part : row;
+  T* to = (T*)a.out[0];
+  if (second) to = (T*)a.out[1];
   if (to == nullptr || (a.row_part > 0 && rr >= a.rows)) return;
-  const float* from = a.partial + row * a.pitch + n;
-  const size_t part = (size_t)a.M * a.pitch;
+  const size_t size = (size_t)rows * cols;
+  const float* from = g.partial + rest * size + q;
   f32x4 v = *reinterpret_cast<const f32x4*>(from);
 #pragma unroll 4
-  for (int p = 1; p < a.parts; ++p) v += *reinterpret_cast<const f32x4*>(from + p * part);
-  to += rr * a.ldo + n;
+  for (int p = 1; p < g.parts; ++p) v += *reinterpret_cast<const f32x4*>(from + p * tail * size);
+  to += (size_t)rr * a.ldo + n;
 #pragma unroll
   for (int i = 0; i < 4; ++i)
-    if (n + i < a.N) to[i] = to_elem<E>(v[i] + (a.bias != nullptr ? E::to_f32(((const T*)a.bias)[n + i]) : 0.0f));
+    if (a.bias[0] != nullptr && n + i < a.N) v[i] += E::to_f32(((const T*)a.bias[0])[n + i]);
+  if (a.aligned && n + 4 <= a.N) {
+    if constexpr (sizeof(T) == 4) *reinterpret_cast<f32x4*>(to) = v;
+    else *reinterpret_cast<u32x2*>(to) = u32x2{Mx<E>::pack2(v[0], v[1]), Mx<E>::pack2(v[2], v[3])};
+  } else {
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+      if (n + i < a.N) to[i] = to_elem<E>(v[i]);
+  }
 }
 
 // partial[part][c] = sum over the part's rows of in[row][c]: a block takes 64 columns, four rows at a time.
@@ -97,6 +102,16 @@ __global__ __launch_bounds__(256) void ffn_column_sum_kernel(const void* in, lon
     partial[(size_t)blockIdx.y * pitch + c] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
   }
 }
+// out[c] = sum over the parts of partial[part][c], in their order, rounded once
+template <class E>
+__global__ __launch_bounds__(256) void ffn_column_total_kernel(const float* partial, int parts, int cols, int pitch, void* out) {
+  const int c = blockIdx.x * 256 + threadIdx.x;
+  if (c >= cols) return;
+  float v = 0.0f;
+#pragma unroll 8
+  for (int p = 0; p < parts; ++p) v += partial[(size_t)p * pitch + c];
+  ((typename E::T*)out)[c] = to_elem<E>(v);
+}
 constexpr int kSumRows = 512;      // rows of a part, at least; at most 64 parts
 int column_parts(int rows) { return std::min(64, (rows + kSumRows - 1) / kSumRows); }
 
@@ -108,18 +123,19 @@ struct Plan {
   size_t h, dgu, partial, total;
 };
 struct Products {
-  FfnTile gate, down, dh, dx, dw_in, dw_down;
+  FfnTile gate, down, dh, dx, dw;
 };
 int steps_of(const FfnBlock& b, int k) { return (k * b.es() + 127) / 128; }
 Products products(const FfnBlock& b) {
   const int pitch = ffn_pitch(b.F), es = b.es();
-  auto tile = [&](long long M, long long N, int k, bool split, bool gated) {
-    return ffn_tile(M, N, steps_of(b, k), es, split, gated, kComputeUnits);
+  auto tile = [&](long long M, long long N, long long M2, long long N2, int k, bool split, bool gated) {
+    return ffn_tile(M, N, M2, N2, steps_of(b, k), es, split, gated, kComputeUnits);
   };
-  return Products{tile(b.T, pitch, b.C, false, true), tile(b.T, b.C, b.F, true, false), tile(b.T, pitch, b.C, false, false),
-                  tile(b.T, b.C, 2 * pitch, true, false), tile(2 * pitch, b.C, b.T, true, false), tile(b.C, b.F, b.T, true, false)};
+  return Products{tile(b.T, pitch, 0, 0, b.C, false, true), tile(b.T, b.C, 0, 0, b.F, true, false), tile(b.T, pitch, 0, 0, b.C, false, false),
+                  tile(b.T, b.C, 0, 0, 2 * pitch, true, false), tile(2 * pitch, b.C, b.C, b.F, b.T, true, false)};
 }
-size_t partial_bytes(const FfnTile& t, long long M, int N) { return t.splits > 1 ? (size_t)t.splits * M * round_up(N, 8) * 4 : 0; }
+int tiles_of(const FfnTile& t, long long M, long long N) { return (int)((M + t.rows - 1) / t.rows * ((N + t.cols - 1) / t.cols)); }
+size_t partial_bytes(const FfnTile& t, int tiles) { return t.parts > 1 ? (size_t)(tiles - t.full) * t.parts * t.rows * t.cols * 4 : 0; }
 
 Plan make_plan(const FfnBlock& b, bool backward) {
   const size_t es = b.es(), pitch = ffn_pitch(b.F), C = round_up(b.C, b.unit()), F = round_up(b.F, b.unit());
@@ -140,10 +156,10 @@ Plan make_plan(const FfnBlock& b, bool backward) {
   else w.h = take((size_t)b.T * pitch * (b.T <= kFfnFewRows ? 4 : es));
   size_t part = 0;
   if (backward) {
-    part = std::max({partial_bytes(p.dx, b.T, b.C), partial_bytes(p.dw_in, 2 * (long long)pitch, b.C), partial_bytes(p.dw_down, b.C, b.F),
+    part = std::max({partial_bytes(p.dx, tiles_of(p.dx, b.T, b.C)), partial_bytes(p.dw, tiles_of(p.dw, 2 * pitch, b.C) + tiles_of(p.dw, b.C, b.F)),
                      (size_t)column_parts(b.T) * std::max<size_t>(2 * pitch, round_up(b.C, 8)) * 4});
   } else {
-    part = partial_bytes(p.down, b.T, b.C);
+    part = partial_bytes(p.down, tiles_of(p.down, b.T, b.C));
   }
   w.partial = take(part);
   w.total = std::max(at, kAlign);
@@ -198,41 +214,41 @@ struct Stager {
   }
 };
 
-hipError_t launch_sum(int dtype, const SumArgs& a, hipStream_t st) {
-  const long long threads = (long long)a.M * ((a.N + 3) / 4);
-  const dim3 grid((unsigned)((threads + 255) / 256));
-  if (dtype == 0) ffn_sum_kernel<ElemF32><<<grid, dim3(256), 0, st>>>(a);
-  else if (dtype == 1) ffn_sum_kernel<ElemF16><<<grid, dim3(256), 0, st>>>(a);
-  else ffn_sum_kernel<ElemBF16><<<grid, dim3(256), 0, st>>>(a);
+hipError_t launch_group(const FfnBlock& b, FfnGroup& g, FfnForm form, FfnEpilogue epi, const FfnTile& t, float* partial, hipStream_t st) {
+  const int cols = epi == FfnEpilogue::kGate ? t.cols / 2 : t.cols;
+  int tiles[2] = {0, 0};
+  for (int i = 0; i < 2; ++i) {
+    FfnProduct& a = g.p[i];
+    const int N = epi == FfnEpilogue::kStore ? a.N : a.pitch;      // zeros behind the hidden width
+    a.grid_m = (a.M + t.rows - 1) / t.rows, a.grid_n = (N + cols - 1) / cols;
+    a.aligned = ((uintptr_t)a.out[0] & 15) == 0 && ((uintptr_t)a.out[1] & 15) == 0 && a.ldo % b.unit() == 0;
+    tiles[i] = a.grid_m * a.grid_n;
+  }
+  g.first = tiles[0], g.tiles = tiles[0] + tiles[1], g.parts = t.parts, g.each = t.each, g.partial = partial;
+  g.full = t.parts > 1 ? t.full : g.tiles;
+  const hipError_t err = b.dtype == 0   ? launch_ffn_product_f32(g, form, epi, t.rows, t.cols, st)
+                         : b.dtype == 1 ? launch_ffn_product_f16(g, form, epi, t.rows, t.cols, st)
+                                        : launch_ffn_product_bf16(g, form, epi, t.rows, t.cols, st);
+  if (err != hipSuccess || g.full == g.tiles) return err;
+  const dim3 grid((unsigned)(t.rows * t.cols / 1024), (unsigned)(g.tiles - g.full)), block(256);
+  if (b.dtype == 0) ffn_sum_kernel<ElemF32><<<grid, block, 0, st>>>(g, t.rows, t.cols);
+  else if (b.dtype == 1) ffn_sum_kernel<ElemF16><<<grid, block, 0, st>>>(g, t.rows, t.cols);
+  else ffn_sum_kernel<ElemBF16><<<grid, block, 0, st>>>(g, t.rows, t.cols);
   return hipGetLastError();
-}
-
-hipError_t launch_product(int dtype, const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st) {
-  if (dtype == 0) return launch_ffn_product_f32(a, form, epi, t, st);
-  return dtype == 1 ? launch_ffn_product_f16(a, form, epi, t, st) : launch_ffn_product_bf16(a, form, epi, t, st);
-}
-
-// kStore, over parts of k where the tile says so
-hipError_t store_product(const FfnBlock& b, FfnProduct a, FfnForm form, const FfnTile& t, float* partial, hipStream_t st) {
-  a.aligned = ((uintptr_t)a.out[0] & 15) == 0 && ((uintptr_t)a.out[1] & 15) == 0 && a.ldo % b.unit() == 0;
-  const int steps = steps_of(b, a.K);
-  a.splits = t.splits, a.split_steps = (steps + t.splits - 1) / t.splits;
-  if (t.splits == 1) return launch_product(b.dtype, a, form, FfnEpilogue::kStore, t, st);
-  a.partial = partial, a.pitch = round_up(a.N, 8);
-  const hipError_t err = launch_product(b.dtype, a, form, FfnEpilogue::kPartial, t, st);
-  if (err != hipSuccess) return err;
-  return launch_sum(b.dtype, SumArgs{partial, t.splits, a.M, a.N, a.pitch, a.row_part, a.rows, a.ldo, a.out[0], a.out[1], a.bias[0]}, st);
 }
 
 hipError_t column_sums(int dtype, const void* in, long long ld, int rows, int cols, float* partial, void* out, hipStream_t st) {
   const int parts = column_parts(rows), each = (rows + parts - 1) / parts, pitch = round_up(cols, 8);
-  const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)parts), block(256);
+  const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)parts), block(256), total((unsigned)((cols + 255) / 256));
   if (dtype == 0) ffn_column_sum_kernel<ElemF32><<<grid, block, 0, st>>>(in, ld, rows, cols, each, pitch, partial);
   else if (dtype == 1) ffn_column_sum_kernel<ElemF16><<<grid, block, 0, st>>>(in, ld, rows, cols, each, pitch, partial);
   else ffn_column_sum_kernel<ElemBF16><<<grid, block, 0, st>>>(in, ld, rows, cols, each, pitch, partial);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  return launch_sum(dtype, SumArgs{partial, parts, 1, cols, pitch, 0, 0, cols, out, nullptr, nullptr}, st);
+  if (dtype == 0) ffn_column_total_kernel<ElemF32><<<total, block, 0, st>>>(partial, parts, cols, pitch, out);
+  else if (dtype == 1) ffn_column_total_kernel<ElemF16><<<total, block, 0, st>>>(partial, parts, cols, pitch, out);
+  else ffn_column_total_kernel<ElemBF16><<<total, block, 0, st>>>(partial, parts, cols, pitch, out);
+  return hipGetLastError();
 }
 
 }  // namespace
@@ -294,20 +310,21 @@ hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* workspace, hipSt
   }
   AA_TRY(stage.launch(st));
   char* keep = (char*)saved;
-  FfnProduct g{};
+  FfnGroup gate{}, down{};
+  FfnProduct& g = gate.p[0];
   g.a = x.p, g.lda = x.ld, g.b[0] = wg2.p, g.b[1] = wu.p, g.ldb = wg2.ld;
-  g.M = b.T, g.N = b.F, g.K = round_up(b.C, unit), g.splits = 1, g.split_steps = steps_of(b, g.K);
+  g.M = b.T, g.N = b.F, g.K = round_up(b.C, unit);
   g.bias[0] = b.b_gate, g.bias[1] = b.b_up, g.pitch = pitch, g.hidden = b.F, g.activation = b.activation;
   g.h = keep ? keep + s.h : ws + w.h;
   if (keep) {
     g.p_hi = (uint16_t*)(keep + s.p_hi), g.q_hi = (uint16_t*)(keep + s.q_hi);
     g.p_lo = (uint8_t*)(keep + s.p_lo), g.q_lo = (uint8_t*)(keep + s.q_lo);
   }
-  AA_TRY(launch_product(b.dtype, g, FfnForm::kKK, FfnEpilogue::kGate, p.gate, st));
-  FfnProduct d{};
+  AA_TRY(launch_group(b, gate, FfnForm::kKK, FfnEpilogue::kGate, p.gate, nullptr, st));
+  FfnProduct& d = down.p[0];
   d.a = g.h, d.lda = pitch, d.b[0] = wd.p, d.ldb = wd.ld, d.M = b.T, d.N = b.C, d.K = round_up(b.F, unit);
   d.out[0] = b.y, d.ldo = b.ldy, d.bias[0] = b.b_down;
-  return store_product(b, d, FfnForm::kKK, p.down, (float*)(ws + w.partial), st);
+  return launch_group(b, down, FfnForm::kKK, FfnEpilogue::kStore, p.down, (float*)(ws + w.partial), st);
 }
 
 hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace, hipStream_t st) {
@@ -336,30 +353,32 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
   }
   AA_TRY(stage.launch(st));
   if (want_dx || dw_in || b.db_gate || b.db_up) {
-    FfnProduct g{};
+    FfnGroup group{};
+    FfnProduct& g = group.p[0];
     g.a = dy.p, g.lda = dy.ld, g.b[0] = wd.p, g.ldb = wd.ld, g.b_m = F, g.b_rows = b.C, g.M = b.T, g.N = b.F, g.K = C;
-    g.splits = 1, g.split_steps = steps_of(b, C), g.pitch = pitch, g.hidden = b.F, g.out[0] = dgu;
+    g.pitch = pitch, g.hidden = b.F, g.out[0] = dgu;
     g.p_hi = (uint16_t*)(keep + s.p_hi), g.q_hi = (uint16_t*)(keep + s.q_hi);
     g.p_lo = (uint8_t*)(keep + s.p_lo), g.q_lo = (uint8_t*)(keep + s.q_lo);
-    AA_TRY(launch_product(b.dtype, g, FfnForm::kKM, FfnEpilogue::kGateGrad, p.dh, st));
+    AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kGateGrad, p.dh, nullptr, st));
   }
   if (want_dx) {
-    FfnProduct d{};
+    FfnGroup group{};
+    FfnProduct& d = group.p[0];
     d.a = dgu, d.lda = 2 * (long long)pitch, d.b[0] = wg.p, d.b[1] = wu.p, d.ldb = wg.ld, d.b_m = C, d.b_rows = b.F, d.b_parts = 2;
     d.k_part = pitch, d.M = b.T, d.N = b.C, d.K = 2 * pitch, d.out[0] = b.dx, d.ldo = b.lddx;
-    AA_TRY(store_product(b, d, FfnForm::kKM, p.dx, partial, st));
+    AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kStore, p.dx, partial, st));
   }
-  if (dw_in) {
-    FfnProduct d{};
+  if (dw_in || b.dw_down) {      // one launch: together they come nearer to whole rounds of the compute units
+    FfnGroup group{};
+    FfnProduct &d = group.p[0], &e = group.p[1];
     d.a = dgu, d.lda = 2 * (long long)pitch, d.a_m = 2 * pitch, d.b[0] = x.p, d.ldb = x.ld, d.b_m = C, d.b_rows = b.T;
-    d.M = 2 * pitch, d.N = b.C, d.K = b.T, d.row_part = pitch, d.rows = b.F, d.out[0] = b.dw_gate, d.out[1] = b.dw_up, d.ldo = b.C;
-    AA_TRY(store_product(b, d, FfnForm::kMM, p.dw_in, partial, st));
-  }
-  if (b.dw_down) {
-    FfnProduct d{};
-    d.a = dy.p, d.lda = dy.ld, d.a_m = C, d.b[0] = keep + s.h, d.ldb = pitch, d.b_m = pitch, d.b_rows = b.T;
-    d.M = b.C, d.N = b.F, d.K = b.T, d.out[0] = b.dw_down, d.ldo = b.F;
-    AA_TRY(store_product(b, d, FfnForm::kMM, p.dw_down, partial, st));
+    d.M = dw_in ? 2 * pitch : 0, d.N = b.C, d.K = b.T, d.row_part = pitch, d.rows = b.F, d.out[0] = b.dw_gate, d.out[1] = b.dw_up, d.ldo = b.C;
+    e.a = dy.p, e.lda = dy.ld, e.a_m = C, e.b[0] = keep + s.h, e.ldb = pitch, e.b_m = pitch, e.b_rows = b.T;
+    e.M = b.dw_down ? b.C : 0, e.N = b.F, e.K = b.T, e.out[0] = b.dw_down, e.ldo = b.F;
+    FfnTile t = p.dw;
+    if (!dw_in || !b.dw_down)      // one of them alone: its own tiles, no more than the plan has room for
+      t = ffn_tile(e.M > 0 ? e.M : d.M, e.M > 0 ? e.N : d.N, 0, 0, steps_of(b, b.T), b.es(), false, false, kComputeUnits);
+    AA_TRY(launch_group(b, group, FfnForm::kMM, FfnEpilogue::kStore, t, partial, st));
   }
   if (b.db_gate) AA_TRY(column_sums(b.dtype, dgu, 2 * (long long)pitch, b.T, b.F, partial, b.db_gate, st));
   if (b.db_up) AA_TRY(column_sums(b.dtype, (const char*)dgu + (size_t)pitch * b.es(), 2 * (long long)pitch, b.T, b.F, partial, b.db_up, st));

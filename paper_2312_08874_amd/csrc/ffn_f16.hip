@@ -3,8 +3,8 @@
 #include "ffn_rows_kernels.inc"
 
 namespace aa {
-hipError_t launch_ffn_product_f16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st) {
-  return product<ElemF16>(a, form, epi, t, st);
+hipError_t launch_ffn_product_f16(const FfnGroup& g, FfnForm form, FfnEpilogue epi, int rows, int cols, hipStream_t st) {
+  return product<ElemF16>(g, form, epi, rows, cols, st);
 }
 hipError_t launch_ffn_rows_f16(const FfnRows& a, bool gate, int waves, hipStream_t st) { return rows_product<ElemF16>(a, gate, waves, st); }
 }  // namespace aa

@@ -135,9 +135,9 @@ size_t rotary_partial_floats(const RotaryArgs& a);
 hipError_t launch_rotary(int dtype, RotaryArgs& a, const RotaryShape& s, RotaryMode mode, float* dw_q, float* dw_k, hipStream_t st);
 
 // --- the gated feed-forward block: ffn.hip, and one unit per element type ---
-hipError_t launch_ffn_product_f32(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
-hipError_t launch_ffn_product_f16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
-hipError_t launch_ffn_product_bf16(const FfnProduct& a, FfnForm form, FfnEpilogue epi, const FfnTile& t, hipStream_t st);
+hipError_t launch_ffn_product_f32(const FfnGroup& g, FfnForm form, FfnEpilogue epi, int rows, int cols, hipStream_t st);
+hipError_t launch_ffn_product_f16(const FfnGroup& g, FfnForm form, FfnEpilogue epi, int rows, int cols, hipStream_t st);
+hipError_t launch_ffn_product_bf16(const FfnGroup& g, FfnForm form, FfnEpilogue epi, int rows, int cols, hipStream_t st);
 hipError_t launch_ffn_rows_f32(const FfnRows& a, bool gate, int waves, hipStream_t st);
 hipError_t launch_ffn_rows_f16(const FfnRows& a, bool gate, int waves, hipStream_t st);
 hipError_t launch_ffn_rows_bf16(const FfnRows& a, bool gate, int waves, hipStream_t st);

@@ -85,21 +85,24 @@ def test_struct_layouts():
 def rule(tmp_path_factory):
     at = tmp_path_factory.mktemp("rule")
     (at / "r.cpp").write_text('''#include "%s/paper_2312_08874_amd/csrc/ffn.h"
-extern "C" void tile(long long M, long long N, int steps, int es, int split, int gated, int* out) {
-  const aa::FfnTile t = aa::ffn_tile(M, N, steps, es, split, gated, 256);
-  out[0] = t.rows, out[1] = t.cols, out[2] = t.splits;
+extern "C" void tile(long long M, long long N, long long M2, long long N2, int steps, int es, int split, int gated, int* out) {
+  const aa::FfnTile t = aa::ffn_tile(M, N, M2, N2, steps, es, split, gated, 256);
+  out[0] = t.rows, out[1] = t.cols, out[2] = t.full, out[3] = t.parts, out[4] = t.each;
 }
 extern "C" int pitch(int hidden) { return aa::ffn_pitch(hidden); }
+extern "C" void place(unsigned at, unsigned m, unsigned n, int* out) { aa::ffn_place(at, m, n, out[0], out[1]); }
+extern "C" unsigned run(unsigned L, unsigned count) { return aa::ffn_run(L, count); }
 ''' % ROOT)
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-o", str(at / "r.so"), str(at / "r.cpp")], check=True)
     lib = ctypes.CDLL(str(at / "r.so"))
+    lib.tile.argtypes = [ctypes.c_longlong] * 4 + [ctypes.c_int] * 4 + [ctypes.c_void_p]
+    return lib
 
-    def call(M, N, steps, es, split, gated):
-        out = (ctypes.c_int * 3)()
-        lib.tile(ctypes.c_longlong(M), ctypes.c_longlong(N), steps, es, int(split), int(gated), out)
-        return tuple(out)
-    call.pitch = lib.pitch
-    return call
+
+def tile(rule, M, N, steps, es, split, gated, M2=0, N2=0):
+    out = (ctypes.c_int * 5)()
+    rule.tile(M, N, M2, N2, steps, es, int(split), int(gated), out)
+    return tuple(out)
 
 
 def test_tiles_and_parts(rule):
@@ -109,10 +112,29 @@ def test_tiles_and_parts(rule):
             for steps in (1, 3, 8, 40, 1000):
                 for es in (2, 4):
                     for split, gated in ((False, True), (True, False)):
-                        rows, cols, parts = rule(M, N, steps, es, split, gated)
-                        assert rows == cols and rows in ((64, 128, 256) if es == 2 else (64, 128))
-                        assert parts >= 1 and (split or parts == 1)
-                        each = (steps + parts - 1) // parts      # every part has steps of its own
-                        assert (parts - 1) * each < steps
-    assert rule(8192, 5504, 32, 2, False, True)[0] == 256
-    assert rule(1, 64, 8, 2, True, False)[0] == 64
+                        for M2 in (0, 300) if split else (0,):
+                            rows, cols, full, parts, each = tile(rule, M, N, steps, es, split, gated, M2, 700)
+                            assert (rows, cols) in (((256, 256), (256, 128), (128, 128), (64, 64)) if es == 2 else ((128, 128), (64, 64)))
+                            of = cols // 2 if gated else cols
+                            tiles = -(-M // rows) * -(-N // of) + (-(-M2 // rows) * -(-700 // of))
+                            assert parts >= 1 and (split or parts == 1) and 0 <= full <= tiles
+                            if parts > 1:      # every part has steps of its own, and the tail's launch fits its grid
+                                assert full < tiles and tiles - full < 65536
+                                assert (parts - 1) * each < steps <= parts * each
+                            else:
+                                assert full == tiles
+    assert tile(rule, 8192, 5504, 32, 2, False, True)[:2] == (256, 256)
+    assert tile(rule, 1, 64, 8, 2, True, False)[0] == 64
+
+
+def test_every_tile_has_one_block(rule):
+    for m, n in ((1, 1), (7, 3), (8, 8), (9, 5), (23, 17), (64, 2)):
+        seen, out = set(), (ctypes.c_int * 2)()
+        for at in range(m * n):
+            rule.place(at, m, n, out)
+            assert 0 <= out[0] < m and 0 <= out[1] < n
+            seen.add(tuple(out))
+        assert len(seen) == m * n
+    for count in (1, 7, 8, 9, 255, 256, 300):
+        got = [rule.run(L, count) for L in range((count + 7) // 8 * 8)]
+        assert sorted(x for x in got if x < count) == list(range(count))
