@@ -590,6 +590,12 @@ def agent_broadcast_fwd(Q, A, VA, V=None, *, grid=None, params: dict | None = No
     return out
 
 
+def _stream_on(stream, device):
+    """The stream's handle, or that of the current stream of the tensors' device."""
+    import torch
+    return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
+
+
 # --- rotary positions, norms of queries and keys ---
 
 ROPE_PAIRINGS = {"adjacent": 0, "halves": 1, "axis_halves": 2}
@@ -712,7 +718,7 @@ def _check_weights(weights, Q, K):
 def _rope_args(Q, K, rope, out, stream):
     desc, views, outs = _rotary_call(Q, K, rope, (), out, stream)
     (q, k), (qo, ko) = views
-    return (ctypes.byref(desc), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream(stream)), outs, (desc, views)
+    return (ctypes.byref(desc), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream_on(stream, Q.device)), outs, (desc, views)
 
 
 def agent_rope_fwd(Q, K, rope, *, out=None, stream=None):
@@ -735,7 +741,7 @@ def _qk_norm_args(Q, K, rope, weights, eps, out, stream):
     wq, wk, per_head = _check_weights(weights, Q, K)
     norm = aa_qk_norm(_ptr(wq), _ptr(wk), int(per_head), eps)
     (q, k), (qo, ko) = views
-    return (ctypes.byref(desc), ctypes.byref(norm), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream(stream)), outs, \
+    return (ctypes.byref(desc), ctypes.byref(norm), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream_on(stream, Q.device)), outs, \
         (desc, norm, views)
 
 
@@ -765,7 +771,7 @@ def agent_qk_norm_bwd(Q, K, dQ_out, dK_out, rope=None, *, weights=None, eps=1e-6
     (q, k), (gq, gk), (dq, dk) = views
     st = lib().agent_qk_norm_bwd(ctypes.byref(desc), ctypes.byref(norm), _ref(q), _ref(k), _ref(gq), _ref(gk), _ptr(workspace),
                                  0 if workspace is None else workspace.numel() * workspace.element_size(), _ref(dq), _ref(dk),
-                                 _ptr(dw[0]), _ptr(dw[1]), _stream(stream))
+                                 _ptr(dw[0]), _ptr(dw[1]), _stream_on(stream, Q.device))
     _check(st, "agent_qk_norm_bwd")
     grads = {"dq": outs[0], "dk": outs[1], "dw_q": dw[0], "dw_k": dw[1]}
     return {name: t for name, t in grads.items() if t is not None}
@@ -822,7 +828,7 @@ def _ffn_fwd_args(x, w, desc, out, saved, workspace, stream):
     desc.y_stride = _ffn_rows("out", out, x)
     workspace = _ffn_workspace(int(lib().agent_gated_ffn_workspace_bytes(ctypes.byref(desc))), workspace, stream, x.device)
     return (ctypes.byref(desc), x.data_ptr(), ctypes.byref(w), _ptr(saved), workspace.data_ptr(),
-            workspace.numel() * workspace.element_size(), out.data_ptr(), _stream(stream)), workspace
+            workspace.numel() * workspace.element_size(), out.data_ptr(), _stream_on(stream, x.device)), workspace
 
 
 def agent_gated_ffn_fwd(x, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu", save=False,
@@ -868,7 +874,7 @@ def agent_gated_ffn_bwd(x, dy, saved, w_gate, w_up, w_down, *, b_gate=None, b_up
     workspace = _ffn_workspace(int(lib().agent_gated_ffn_bwd_workspace_bytes(ctypes.byref(desc))), workspace, stream, x.device)
     st = lib().agent_gated_ffn_bwd(ctypes.byref(desc), x.data_ptr(), ctypes.byref(w), saved.data_ptr(), dy.data_ptr(),
                                    workspace.data_ptr(), workspace.numel() * workspace.element_size(), _ptr(out.get("dx")),
-                                   ctypes.byref(g), _stream(stream))
+                                   ctypes.byref(g), _stream_on(stream, x.device))
     _check(st, "agent_gated_ffn_bwd")
     return out
 

@@ -75,7 +75,7 @@ aa_status agent_gated_ffn_fwd(const aa_ffn* desc, const void* x, const aa_ffn_we
   if (st != AA_OK) return st;
   if (!x || !w || !w->w_gate || !w->w_up || !w->w_down || !y) return AA_ERR_NULL;
   aa::FfnBlock b = block_of(desc);
-  if (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < aa::ffn_fwd_workspace(b)) return AA_ERR_WORKSPACE;
+  if (!workspace || ((uintptr_t)workspace % kAlign) != 0) return AA_ERR_WORKSPACE;
   if (((uintptr_t)saved % kAlign) != 0) return AA_ERR_WORKSPACE;
   const size_t es = b.es(), C = b.C, F = b.F, in = C * F * es;
   const Range results[] = {{y, ((size_t)(b.T - 1) * b.ldy + C) * es}, {workspace, workspace_bytes}, {saved, aa::ffn_saved_bytes(b)}};
@@ -85,7 +85,9 @@ aa_status agent_gated_ffn_fwd(const aa_ffn* desc, const void* x, const aa_ffn_we
   if (at != AA_OK) return at;
   b.x = x, b.w_gate = w->w_gate, b.b_gate = w->b_gate, b.w_up = w->w_up, b.b_up = w->b_up;
   b.w_down = w->w_down, b.b_down = w->b_down, b.y = y;
-  return aa::launch_ffn_fwd(b, saved, workspace, (hipStream_t)hip_stream) == hipSuccess ? AA_OK : AA_ERR_HIP;
+  bool room;
+  const hipError_t err = aa::launch_ffn_fwd(b, saved, workspace, workspace_bytes, &room, (hipStream_t)hip_stream);
+  return !room ? AA_ERR_WORKSPACE : err == hipSuccess ? AA_OK : AA_ERR_HIP;
 }
 
 aa_status agent_gated_ffn_bwd(const aa_ffn* desc, const void* x, const aa_ffn_weights* w, const void* saved, const void* dy,
@@ -94,7 +96,7 @@ aa_status agent_gated_ffn_bwd(const aa_ffn* desc, const void* x, const aa_ffn_we
   if (st != AA_OK) return st;
   if (!x || !w || !w->w_gate || !w->w_up || !w->w_down || !saved || !dy) return AA_ERR_NULL;
   aa::FfnBlock b = block_of(desc);
-  if (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < aa::ffn_bwd_workspace(b)) return AA_ERR_WORKSPACE;
+  if (!workspace || ((uintptr_t)workspace % kAlign) != 0) return AA_ERR_WORKSPACE;
   if (((uintptr_t)saved % kAlign) != 0) return AA_ERR_WORKSPACE;
   const aa_ffn_grads none{}, *to = g ? g : &none;
   const size_t es = b.es(), C = b.C, F = b.F, in = C * F * es;
@@ -107,7 +109,9 @@ aa_status agent_gated_ffn_bwd(const aa_ffn* desc, const void* x, const aa_ffn_we
   b.x = x, b.w_gate = w->w_gate, b.w_up = w->w_up, b.w_down = w->w_down, b.dy = dy, b.dx = dx;
   b.dw_gate = to->dw_gate, b.dw_up = to->dw_up, b.dw_down = to->dw_down;
   b.db_gate = to->db_gate, b.db_up = to->db_up, b.db_down = to->db_down;
-  return aa::launch_ffn_bwd(b, saved, workspace, (hipStream_t)hip_stream) == hipSuccess ? AA_OK : AA_ERR_HIP;
+  bool room;
+  const hipError_t err = aa::launch_ffn_bwd(b, saved, workspace, workspace_bytes, &room, (hipStream_t)hip_stream);
+  return !room ? AA_ERR_WORKSPACE : err == hipSuccess ? AA_OK : AA_ERR_HIP;
 }
 
 }  // extern "C"

@@ -75,7 +75,12 @@ AA_HOST_DEVICE void ffn_place(unsigned at, unsigned grid_m, unsigned grid_n, int
 AA_HOST_DEVICE unsigned ffn_run(unsigned L, unsigned count) { return (L & 7u) * ((count + 7u) / 8u) + (L >> 3); }
 
 // A few tokens: x -> h (w: gate and up, K = width, N = hidden) and h -> y (w[0]: down, K = hidden, N = width).  Weights [N][K], dense.
-constexpr int kFfnFewRows = 64;
+constexpr int kFfnFewRows = 64;      // most tokens of their kernels
+inline bool ffn_few_rows(int T, int C, int F) {
+  // up to one tile of tokens; to four while the weights are small enough that the other kernels' latency counts (bf16, T tokens,
+  // these and those: 512 x 1365, 64 tokens 18.9 and 21.7 us; 1024 x 2816, 32: 17.7, 20.2, 48: 24.8, 20.5; 2048 x 5504, 24: 33.8, 29.3)
+  return T <= 16 || (T <= kFfnFewRows && (long long)T * C * F <= 100000000ll);
+}
 struct FfnRows {
   const void *w[2], *x, *bias[2];
   long long ldx, ldy;
@@ -135,11 +140,14 @@ inline FfnTile ffn_tile(long long M, long long N, long long M2, long long N2, in
     };
     consider(tiles, 1, steps);
     if (!split) continue;
-    const long long full = tiles / room * room;      // whole rounds
-    if (full == tiles) continue;
-    for (int parts = 2; parts <= 64 && steps / parts >= 2; ++parts) {
-      const int each = (steps + parts - 1) / parts;
-      if ((steps + each - 1) / each == parts) consider(full, parts, each);
+    const long long full = tiles / room * room, tail = tiles - full;      // whole rounds, and what is left
+    if (tail == 0) continue;
+    int before = 1;
+    for (int rounds = 1; rounds <= 3; ++rounds) {      // as many parts as fill one, two or three rounds
+      const int most = (int)std::min<long long>(std::min(64, steps / 2), room * rounds / tail);
+      if (most <= before) continue;
+      const int each = (steps + most - 1) / most, parts = (steps + each - 1) / each;      // every part has steps of its own
+      if (parts > before) consider(full, parts, each), before = parts;
     }
   }
   return best;

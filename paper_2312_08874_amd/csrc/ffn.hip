@@ -116,53 +116,63 @@ constexpr int kSumRows = 512;      // rows of a part, at least; at most 64 parts
 int column_parts(int rows) { return std::min(64, (rows + kSumRows - 1) / kSumRows); }
 
 // --- workspaces ---
-// Copies of operands whose rows are no whole 16-byte pieces; their room is always kept, since the tensors' addresses are not
-// known to a query.
-struct Plan {
-  size_t x, dy, w_gate, w_up, w_down;      // copies
-  size_t h, dgu, partial, total;
-};
-struct Products {
-  FfnTile gate, down, dh, dx, dw;
-};
 int steps_of(const FfnBlock& b, int k) { return (k * b.es() + 127) / 128; }
-Products products(const FfnBlock& b) {
-  const int pitch = ffn_pitch(b.F), es = b.es();
-  auto tile = [&](long long M, long long N, long long M2, long long N2, int k, bool split, bool gated) {
-    return ffn_tile(M, N, M2, N2, steps_of(b, k), es, split, gated, kComputeUnits);
-  };
-  return Products{tile(b.T, pitch, 0, 0, b.C, false, true), tile(b.T, b.C, 0, 0, b.F, true, false), tile(b.T, pitch, 0, 0, b.C, false, false),
-                  tile(b.T, b.C, 0, 0, 2 * pitch, true, false), tile(2 * pitch, b.C, b.C, b.F, b.T, true, false)};
+FfnTile tile_for(const FfnBlock& b, long long M, long long N, long long M2, long long N2, int k, bool split, bool gated) {
+  return ffn_tile(M, N, M2, N2, steps_of(b, k), b.es(), split, gated, kComputeUnits);
 }
 int tiles_of(const FfnTile& t, long long M, long long N) { return (int)((M + t.rows - 1) / t.rows * ((N + t.cols - 1) / t.cols)); }
 size_t partial_bytes(const FfnTile& t, int tiles) { return t.parts > 1 ? (size_t)(tiles - t.full) * t.parts * t.rows * t.cols * 4 : 0; }
 
-Plan make_plan(const FfnBlock& b, bool backward) {
-  const size_t es = b.es(), pitch = ffn_pitch(b.F), C = round_up(b.C, b.unit()), F = round_up(b.F, b.unit());
-  const Products p = products(b);
-  Plan w{};
+// The products' tiles and where things lie in the workspace.  Copies of operands whose rows are no whole 16-byte pieces have
+// their room always, since the tensors' addresses are not known to a query.
+struct ForwardPlan {
+  FfnTile gate{}, down{};
+  size_t x = 0, w_gate = 0, w_up = 0, w_down = 0, h = 0, partial = 0, total = 0;
+};
+struct BackwardPlan {
+  FfnTile dh{}, dx{}, dw{};
+  size_t x = 0, dy = 0, w_gate = 0, w_up = 0, w_down = 0, dgu = 0, partial = 0, total = 0;
+};
+struct Regions {
   size_t at = 0;
-  auto take = [&](size_t bytes) {
+  size_t take(size_t bytes) {
     const size_t o = at;
     at += align_up(bytes);
     return o;
-  };
-  w.x = take((size_t)b.T * C * es);
-  if (backward) w.dy = take((size_t)b.T * C * es);
-  w.w_gate = take((size_t)b.F * C * es);
-  w.w_up = take((size_t)b.F * C * es);
-  w.w_down = take((size_t)b.C * F * es);
-  if (backward) w.dgu = take((size_t)b.T * 2 * pitch * es);
-  else w.h = take((size_t)b.T * pitch * (b.T <= kFfnFewRows ? 4 : es));
-  size_t part = 0;
-  if (backward) {
-    part = std::max({partial_bytes(p.dx, tiles_of(p.dx, b.T, b.C)), partial_bytes(p.dw, tiles_of(p.dw, 2 * pitch, b.C) + tiles_of(p.dw, b.C, b.F)),
-                     (size_t)column_parts(b.T) * std::max<size_t>(2 * pitch, round_up(b.C, 8)) * 4});
-  } else {
-    part = partial_bytes(p.down, tiles_of(p.down, b.T, b.C));
   }
-  w.partial = take(part);
-  w.total = std::max(at, kAlign);
+};
+
+ForwardPlan forward_plan(const FfnBlock& b) {
+  const size_t es = b.es(), pitch = ffn_pitch(b.F), C = round_up(b.C, b.unit()), F = round_up(b.F, b.unit());
+  ForwardPlan w;
+  Regions r;
+  if (ffn_few_rows(b.T, b.C, b.F)) {
+    w.h = r.take((size_t)b.T * pitch * 4);      // fp32, or two terms
+    w.total = r.at;
+    return w;
+  }
+  w.gate = tile_for(b, b.T, pitch, 0, 0, b.C, false, true), w.down = tile_for(b, b.T, b.C, 0, 0, b.F, true, false);
+  w.x = r.take((size_t)b.T * C * es);
+  w.w_gate = r.take((size_t)b.F * C * es), w.w_up = r.take((size_t)b.F * C * es), w.w_down = r.take((size_t)b.C * F * es);
+  w.h = r.take((size_t)b.T * pitch * es);
+  w.partial = r.take(partial_bytes(w.down, tiles_of(w.down, b.T, b.C)));
+  w.total = r.at;
+  return w;
+}
+
+BackwardPlan backward_plan(const FfnBlock& b) {
+  const size_t es = b.es(), pitch = ffn_pitch(b.F), C = round_up(b.C, b.unit()), F = round_up(b.F, b.unit());
+  BackwardPlan w;
+  Regions r;
+  w.dh = tile_for(b, b.T, pitch, 0, 0, b.C, false, false), w.dx = tile_for(b, b.T, b.C, 0, 0, 2 * pitch, true, false);
+  w.dw = tile_for(b, 2 * pitch, b.C, b.C, b.F, b.T, true, false);
+  w.x = r.take((size_t)b.T * C * es), w.dy = r.take((size_t)b.T * C * es);
+  w.w_gate = r.take((size_t)b.F * C * es), w.w_up = r.take((size_t)b.F * C * es), w.w_down = r.take((size_t)b.C * F * es);
+  w.dgu = r.take((size_t)b.T * 2 * pitch * es);
+  w.partial = r.take(std::max({partial_bytes(w.dx, tiles_of(w.dx, b.T, b.C)),
+                               partial_bytes(w.dw, tiles_of(w.dw, 2 * pitch, b.C) + tiles_of(w.dw, b.C, b.F)),
+                               (size_t)column_parts(b.T) * std::max<size_t>(2 * pitch, round_up(b.C, 8)) * 4}));
+  w.total = r.at;
   return w;
 }
 
@@ -196,11 +206,10 @@ struct Stager {
   char* ws;
   CopyJobs jobs{};
   Rows operand(const void* p, long long ld, int rows, int cols, size_t room) {
-    const int es = b.es(), unit = b.unit();
+    const int unit = b.unit();
     if (((uintptr_t)p & 15) == 0 && ld % unit == 0 && cols % unit == 0) return Rows{p, ld};
     CopyJob& j = jobs.job[jobs.count++];
     j = CopyJob{p, ws + room, ld, rows, cols, round_up(cols, unit)};
-    (void)es;
     return Rows{j.dst, j.pitch};
   }
   hipError_t launch(hipStream_t st) {
@@ -254,8 +263,8 @@ hipError_t column_sums(int dtype, const void* in, long long ld, int rows, int co
 }  // namespace
 
 size_t ffn_saved_bytes(const FfnBlock& b) { return saved_plan(b).total; }
-size_t ffn_fwd_workspace(const FfnBlock& b) { return make_plan(b, false).total; }
-size_t ffn_bwd_workspace(const FfnBlock& b) { return make_plan(b, true).total; }
+size_t ffn_fwd_workspace(const FfnBlock& b) { return forward_plan(b).total; }
+size_t ffn_bwd_workspace(const FfnBlock& b) { return backward_plan(b).total; }
 
 #define AA_TRY(call)                          \
   do {                                        \
@@ -287,11 +296,12 @@ hipError_t few_rows_fwd(const FfnBlock& b, char* keep, void* h, hipStream_t st) 
 
 }  // namespace
 
-hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* workspace, hipStream_t st) {
+hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* workspace, size_t bytes, bool* room, hipStream_t st) {
   char* ws = (char*)workspace;
-  const Plan w = make_plan(b, false);
-  if (b.T <= kFfnFewRows) return few_rows_fwd(b, (char*)saved, ws + w.h, st);
-  const Products p = products(b);
+  const ForwardPlan w = forward_plan(b);
+  *room = bytes >= w.total;
+  if (!*room) return hipSuccess;
+  if (ffn_few_rows(b.T, b.C, b.F)) return few_rows_fwd(b, (char*)saved, ws + w.h, st);
   const Saved s = saved_plan(b);
   const int pitch = ffn_pitch(b.F), unit = b.unit();
   Stager stage{b, ws};
@@ -320,17 +330,18 @@ hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* workspace, hipSt
     g.p_hi = (uint16_t*)(keep + s.p_hi), g.q_hi = (uint16_t*)(keep + s.q_hi);
     g.p_lo = (uint8_t*)(keep + s.p_lo), g.q_lo = (uint8_t*)(keep + s.q_lo);
   }
-  AA_TRY(launch_group(b, gate, FfnForm::kKK, FfnEpilogue::kGate, p.gate, nullptr, st));
+  AA_TRY(launch_group(b, gate, FfnForm::kKK, FfnEpilogue::kGate, w.gate, nullptr, st));
   FfnProduct& d = down.p[0];
   d.a = g.h, d.lda = pitch, d.b[0] = wd.p, d.ldb = wd.ld, d.M = b.T, d.N = b.C, d.K = round_up(b.F, unit);
   d.out[0] = b.y, d.ldo = b.ldy, d.bias[0] = b.b_down;
-  return launch_group(b, down, FfnForm::kKK, FfnEpilogue::kStore, p.down, (float*)(ws + w.partial), st);
+  return launch_group(b, down, FfnForm::kKK, FfnEpilogue::kStore, w.down, (float*)(ws + w.partial), st);
 }
 
-hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace, hipStream_t st) {
+hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace, size_t bytes, bool* room, hipStream_t st) {
   char* ws = (char*)workspace;
-  const Plan w = make_plan(b, true);
-  const Products p = products(b);
+  const BackwardPlan w = backward_plan(b);
+  *room = bytes >= w.total;
+  if (!*room) return hipSuccess;
   const Saved s = saved_plan(b);
   const int pitch = ffn_pitch(b.F), unit = b.unit(), C = round_up(b.C, unit), F = round_up(b.F, unit);
   const char* keep = (const char*)saved;
@@ -359,14 +370,14 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
     g.pitch = pitch, g.hidden = b.F, g.out[0] = dgu;
     g.p_hi = (uint16_t*)(keep + s.p_hi), g.q_hi = (uint16_t*)(keep + s.q_hi);
     g.p_lo = (uint8_t*)(keep + s.p_lo), g.q_lo = (uint8_t*)(keep + s.q_lo);
-    AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kGateGrad, p.dh, nullptr, st));
+    AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kGateGrad, w.dh, nullptr, st));
   }
   if (want_dx) {
     FfnGroup group{};
     FfnProduct& d = group.p[0];
     d.a = dgu, d.lda = 2 * (long long)pitch, d.b[0] = wg.p, d.b[1] = wu.p, d.ldb = wg.ld, d.b_m = C, d.b_rows = b.F, d.b_parts = 2;
     d.k_part = pitch, d.M = b.T, d.N = b.C, d.K = 2 * pitch, d.out[0] = b.dx, d.ldo = b.lddx;
-    AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kStore, p.dx, partial, st));
+    AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kStore, w.dx, partial, st));
   }
   if (dw_in || b.dw_down) {      // one launch: together they come nearer to whole rounds of the compute units
     FfnGroup group{};
@@ -375,9 +386,9 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
     d.M = dw_in ? 2 * pitch : 0, d.N = b.C, d.K = b.T, d.row_part = pitch, d.rows = b.F, d.out[0] = b.dw_gate, d.out[1] = b.dw_up, d.ldo = b.C;
     e.a = dy.p, e.lda = dy.ld, e.a_m = C, e.b[0] = keep + s.h, e.ldb = pitch, e.b_m = pitch, e.b_rows = b.T;
     e.M = b.dw_down ? b.C : 0, e.N = b.F, e.K = b.T, e.out[0] = b.dw_down, e.ldo = b.F;
-    FfnTile t = p.dw;
+    FfnTile t = w.dw;
     if (!dw_in || !b.dw_down)      // one of them alone: its own tiles, no more than the plan has room for
-      t = ffn_tile(e.M > 0 ? e.M : d.M, e.M > 0 ? e.N : d.N, 0, 0, steps_of(b, b.T), b.es(), false, false, kComputeUnits);
+      t = tile_for(b, e.M > 0 ? e.M : d.M, e.M > 0 ? e.N : d.N, 0, 0, b.T, false, false);
     AA_TRY(launch_group(b, group, FfnForm::kMM, FfnEpilogue::kStore, t, partial, st));
   }
   if (b.db_gate) AA_TRY(column_sums(b.dtype, dgu, 2 * (long long)pitch, b.T, b.F, partial, b.db_gate, st));

@@ -144,8 +144,9 @@ hipError_t launch_ffn_rows_bf16(const FfnRows& a, bool gate, int waves, hipStrea
 size_t ffn_saved_bytes(const FfnBlock& b);
 size_t ffn_fwd_workspace(const FfnBlock& b);
 size_t ffn_bwd_workspace(const FfnBlock& b);
-hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* ws, hipStream_t st);
-hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* ws, hipStream_t st);
+// *room: whether `bytes` is what the query says; nothing is launched if not
+hipError_t launch_ffn_fwd(const FfnBlock& b, void* saved, void* ws, size_t bytes, bool* room, hipStream_t st);
+hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* ws, size_t bytes, bool* room, hipStream_t st);
 
 // --- small-agent regime (n <= 64, d in {32, 64}, fp16 / bf16): MFMA kernels that keep A and V_A in
 //     registers and stream tokens straight from global memory ---
