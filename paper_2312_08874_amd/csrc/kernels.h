@@ -126,9 +126,9 @@ hipError_t launch_forward_f32(const Problem& p, const void* Q, const void* K, co
                               void* out, hipStream_t st);
 
 // --- rotary positions, norms of queries and keys: rotary.hip, and one unit per element type ---
-hipError_t launch_rotary_f32(const RotaryArgs& a, const RotaryShape& s, RotaryMode mode, int chunk, int blocks, hipStream_t st);
-hipError_t launch_rotary_f16(const RotaryArgs& a, const RotaryShape& s, RotaryMode mode, int chunk, int blocks, hipStream_t st);
-hipError_t launch_rotary_bf16(const RotaryArgs& a, const RotaryShape& s, RotaryMode mode, int chunk, int blocks, hipStream_t st);
+hipError_t launch_rotary_f32(const RotaryArgs& a, int ve, const RotaryPlan& p, RotaryMode mode, hipStream_t st);
+hipError_t launch_rotary_f16(const RotaryArgs& a, int ve, const RotaryPlan& p, RotaryMode mode, hipStream_t st);
+hipError_t launch_rotary_bf16(const RotaryArgs& a, int ve, const RotaryPlan& p, RotaryMode mode, hipStream_t st);
 // fp32 scratch of the backward pass (a.partial)
 size_t rotary_partial_floats(const RotaryArgs& a);
 // dw_q, dw_k: gradients of the norm's weights, backward pass alone, null where they are not wanted

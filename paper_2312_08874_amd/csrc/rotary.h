@@ -40,10 +40,10 @@ enum RotaryPairing { kAdjacent = 0, kHalves = 1, kAxisHalves = 2 };
 // channels that the pairing keeps together (adjacent pairs are inside a load, the others in two loads of equal width).
 struct RotaryShape {
   int ve;        // channels of a load
-  int lanes;     // lanes of a row, a power of two; each has `duos` pairs of loads
-  int duos;
+  int lanes;     // lanes of a row, a power of two
+  int duos;      // pairs of loads of a lane
 };
-inline int rotary_duos(int ve) { return ve >= 4 ? 1 : ve == 2 ? 2 : 4; }
+constexpr int rotary_duos(int ve) { return ve >= 4 ? 1 : ve == 2 ? 2 : 4; }
 inline RotaryShape rotary_shape(int es, int d, int pairing, int axes, const int* first, unsigned long long misaligned_bytes) {
   // misaligned_bytes: all addresses and byte strides, or-ed
   for (int ve = 16 / es;; ve /= 2) {
@@ -59,16 +59,39 @@ inline RotaryShape rotary_shape(int es, int d, int pairing, int axes, const int*
   }
 }
 
-// Heads a wave takes for its tokens (their angles are computed once): all, halved while the waves are fewer than four for each of
-// the 1024 SIMDs.
-inline int rotary_heads_per_wave(long long rows, int heads, int lanes) {
-  const long long tiles = (rows * lanes + 63) / 64;
-  int chunk = heads;
-  while (chunk > 1 && tiles * ((heads + chunk - 1) / chunk) < 4096) chunk = (chunk + 1) / 2;
-  return chunk;
-}
+// How a launch shares out its rows.  A block of four waves takes the tokens of 4 / across waves (64 / lanes tokens each), and
+// `across` of its waves take `chunk` heads each, side by side: the angles of a token, which cost as much as two heads or three,
+// are computed once a block.
+struct RotaryPlan {
+  int lanes, shift;      // lanes of a row, and their logarithm
+  int across, chunk;
+  int chunks[2];         // blocks along y: those of the queries, then those of the keys; forward: [0] has the heads of both
+  int tiles, blocks;     // tiles of tokens, blocks along x
+};
 
 // Backward pass: blocks that walk over the tokens (their sums of the weights' gradients are added up by a second kernel).
 constexpr int kRotarySumBlocks = 1024;
+// Waves that a launch is cut into where it can be: four for each of the 1024 SIMDs.
+constexpr long long kRotaryWaves = 4096;
+
+inline RotaryPlan rotary_plan(const RotaryShape& s, long long rows, int heads_q, int heads_k, bool backward, bool one_head) {
+  // one_head (backward): a wave takes one head, whose weights and sums are its own
+  RotaryPlan p{};
+  p.lanes = s.lanes;
+  while (1 << p.shift < s.lanes) ++p.shift;
+  const int most = backward ? std::max(heads_q, heads_k) : heads_q + heads_k;
+  p.across = most >= 3 ? 4 : most;
+  const long long per = (4 / p.across) * (64 / s.lanes);
+  p.tiles = (int)((rows + per - 1) / per);
+  auto count = [&](int chunk, int heads) { return (heads + p.across * chunk - 1) / (p.across * chunk); };
+  auto blocks = [&](int chunk) { return backward ? count(chunk, heads_q) + count(chunk, heads_k) : count(chunk, most); };
+  p.chunk = backward && one_head ? 1 : (most + p.across - 1) / p.across;
+  while (p.chunk > 1 && 4 * (long long)p.tiles * blocks(p.chunk) < kRotaryWaves) p.chunk = (p.chunk + 1) / 2;
+  p.chunks[0] = count(p.chunk, backward ? heads_q : most), p.chunks[1] = backward ? count(p.chunk, heads_k) : 0;
+  p.blocks = p.tiles;
+  if (backward)
+    p.blocks = std::min(p.tiles, std::max(1, kRotarySumBlocks / (one_head ? 1 : std::max(p.chunks[0], p.chunks[1]))));
+  return p;
+}
 
 }  // namespace aa

@@ -1,7 +1,7 @@
 #include "rotary_kernels.inc"
 
 namespace aa {
-hipError_t launch_rotary_f32(const RotaryArgs& a, const RotaryShape& s, RotaryMode mode, int chunk, int blocks, hipStream_t st) {
-  return dispatch<ElemF32>(a, s, mode, chunk, blocks, st);
+hipError_t launch_rotary_f32(const RotaryArgs& a, int ve, const RotaryPlan& p, RotaryMode mode, hipStream_t st) {
+  return dispatch<ElemF32>(a, ve, p, mode, st);
 }
 }  // namespace aa

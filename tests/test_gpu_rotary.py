@@ -318,3 +318,18 @@ def test_many_tokens_take_several_rounds():
     dx, dscale, dw, dw_scale = ref.norm_bwd(q.double().cpu(), w, 1e-6, spec, dy.double().cpu())
     close(got["dq"], dx, ref.eps_of(torch.bfloat16) * dx.abs() + (2.5 * d + 48) * U * dscale + ref.smallest(torch.bfloat16), "dq")
     close(got["dw_q"], dw, (d / 2 + 24 + 160) * U * dw_scale, "dw")
+
+
+@pytest.mark.parametrize("pairing,pairs", [("halves", (8,)), ("adjacent", (8,)), ("adjacent", (5,)), ("axis_halves", (4, 4))])
+def test_channels_that_do_not_turn_stay_as_they_are(pairing, pairs):
+    """Infinities and NaN among them too: a channel beside them is not touched."""
+    from paper_2312_08874_amd import binding
+    gen = torch.Generator().manual_seed(17)
+    x = torch.randn(1, 3, 40, 48, generator=gen).to(torch.bfloat16)
+    n = 2 * sum(pairs)
+    x[..., n::5], x[..., n + 1::5] = float("inf"), float("nan")
+    spec, _ = spec_for(gen, 1, (40,) if len(pairs) == 1 else (5, 8), pairs, pairing)
+    for fn in (binding.agent_rope_fwd, binding.agent_rope_bwd):
+        y = fn(x.cuda(), None, rope_of(binding, spec))[0].cpu()
+        assert torch.equal(y[..., n:].view(torch.int16), x[..., n:].view(torch.int16))
+        assert bool(torch.isfinite(y[..., :n]).all())

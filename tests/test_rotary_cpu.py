@@ -135,7 +135,10 @@ extern "C" void shape(int es, int d, int pairing, int axes, const int* first, un
   const aa::RotaryShape s = aa::rotary_shape(es, d, pairing, axes, first, align);
   out[0] = s.ve, out[1] = s.lanes, out[2] = s.duos;
 }
-extern "C" int heads(long long rows, int heads, int lanes) { return aa::rotary_heads_per_wave(rows, heads, lanes); }
+extern "C" void plan(long long rows, int heads_q, int heads_k, int lanes, int backward, int one_head, int* out) {
+  const aa::RotaryPlan p = aa::rotary_plan({1, lanes, 1}, rows, heads_q, heads_k, backward, one_head);
+  out[0] = p.shift, out[1] = p.across, out[2] = p.chunk, out[3] = p.chunks[0], out[4] = p.chunks[1], out[5] = p.tiles, out[6] = p.blocks;
+}
 ''' % ROOT)
     subprocess.run(["g++", "-std=c++17", "-shared", "-fPIC", "-o", str(at / "r.so"), str(src)], check=True)
     return ctypes.CDLL(str(at / "r.so"))
@@ -171,10 +174,27 @@ def test_shapes_of_the_kernels(rules):
                 assert lanes <= 64 and lanes * duos * 2 * ve >= d and d % ve == 0 and align % (ve * es) == 0
 
 
-def test_heads_of_a_wave(rules):
-    rules.heads.argtypes = [ctypes.c_longlong, ctypes.c_int, ctypes.c_int]
-    assert rules.heads(1, 16, 4) == 1
-    assert rules.heads(1 << 20, 20, 8) == 20
-    for rows in (1, 100, 12544, 16384, 1 << 22):
-        for heads in (1, 3, 16, 40):
-            assert 1 <= rules.heads(rows, heads, 4) <= heads
+def test_launches_cover_every_row(rules):
+    rules.plan.argtypes = [ctypes.c_longlong] + [ctypes.c_int] * 5 + [ctypes.c_void_p]
+
+    def plan(*args):
+        out = (ctypes.c_int * 7)()
+        rules.plan(*args, out)
+        return tuple(out)
+    assert plan(1, 8, 8, 4, 0, 0)[:5] == (2, 4, 1, 4, 0)            # one token: every wave a head of its own
+    assert plan(1 << 20, 16, 4, 8, 0, 0)[:5] == (3, 4, 5, 1, 0)     # many: a block takes all heads of its tokens
+    for rows in (1, 2, 63, 1000, 12544, 70001, 1 << 22, (1 << 31) - 1):
+        for heads in ((1, 0), (1, 1), (2, 1), (3, 3), (16, 4), (40, 0), (7, 300)):
+            for lanes in (1, 4, 64):
+                for backward, one_head in ((0, 0), (1, 0), (1, 1)):
+                    shift, across, chunk, cq, ck, tiles, blocks = plan(rows, *heads, lanes, backward, one_head)
+                    tokens = 4 // across * (64 // lanes)
+                    assert 1 << shift == lanes and across in (1, 2, 4) and chunk >= 1 and (chunk == 1 or not one_head)
+                    assert (tiles - 1) * tokens < rows <= tiles * tokens and 1 <= blocks <= tiles
+                    share = across * chunk
+                    for c, n in ((cq, heads[0]), (ck, heads[1])) if backward else ((cq, sum(heads)), (ck, 0)):
+                        assert (c - 1) * share < n <= c * share
+                    if backward:      # the sums' workspace
+                        assert blocks * (1 if one_head else max(cq, ck)) <= max(1024, sum(heads))
+                    else:
+                        assert blocks == tiles
