@@ -650,39 +650,40 @@ class Rope:
 
 
 def _view(t):
-    st = (0, 0, 0) if t.is_contiguous() else (t.stride(0), t.stride(1), t.stride(2))
-    assert t.is_contiguous() or any(st) or t.numel() == t.shape[3], "a tensor repeated along every axis has no view: make it dense"
-    return aa_view(t.data_ptr(), *st)
+    if t.is_contiguous():
+        return aa_view(t.data_ptr(), 0, 0, 0)
+    st = t.stride()
+    assert st[0] or st[1] or st[2] or t.numel() == t.shape[3], "a tensor repeated along every axis has no view: make it dense"
+    assert st[3] == 1 or t.shape[3] == 1, "channels must lie side by side"
+    return aa_view(t.data_ptr(), st[0], st[1], st[2])
 
 
-def _check_tokens(what, t, like, heads=None):
-    assert t.is_cuda and t.dim() == 4 and t.dtype == like.dtype and t.device == like.device and \
-        (t.stride(3) == 1 or t.shape[3] == 1), what + " must be [B,H,N,d] on one device, in one dtype, channels side by side"
-    assert t.shape[0] == like.shape[0] and t.shape[2:] == like.shape[2:] and (heads is None or t.shape[1] == heads), \
-        what + " has another batch, number of heads, number of tokens or width"
+def _checked_view(what, t, like, shape):
+    assert t.get_device() == like.get_device() and t.dtype == like.dtype and t.shape == shape, \
+        what + " must be %s, on Q's device, in its dtype" % (tuple(shape),)
+    return _view(t)
 
 
-def _rotary_call(Q, K, rope, inputs=(), outputs=None, stream=None):
-    """Descriptor and views of a call: (Q, K), further pairs of `inputs`, and the outputs (fresh where None)."""
-    import torch
-    _check_tokens("Q", Q, Q)
-    if K is not None:
-        _check_tokens("K", K, Q)
+def _rotary_call(Q, K, rope, beside=None, outputs=None, stream=None):
+    """Descriptor and views of a call: (Q, K), the pair `beside` them, and the outputs (fresh where None)."""
+    assert Q.is_cuda and Q.dim() == 4, "Q must be [B,H,N,d] on the GPU"
+    shape = Q.shape
     desc = rope._desc_for(Q) if rope is not None else aa_rotary()
-    desc.batch, desc.heads_q, desc.tokens, desc.d = Q.shape
-    desc.heads_k = K.shape[1] if K is not None else 0
+    desc.batch, desc.heads_q, desc.tokens, desc.d = shape
     desc.dtype = _dtype_code(Q)
-    if outputs is None:
-        outputs = _outputs_like((Q, K), stream)
-    outputs = tuple(outputs)
+    views = [(_view(Q), None)]
+    if K is not None:
+        assert K.dim() == 4, "K must be [B,H,N,d]"
+        shape_k = (shape[0], K.shape[1], shape[2], shape[3])
+        desc.heads_k = shape_k[1]
+        views = [(views[0][0], _checked_view("K", K, Q, shape_k))]
+    fresh = outputs is None
+    outputs = _outputs_like((Q, K), stream) if fresh else tuple(outputs)
     assert len(outputs) == 2 and (outputs[1] is None) == (K is None), "results for Q and, where there is one, for K"
-    for pair in tuple(inputs) + (outputs,):
-        for name, t, like in (("the tensor beside Q", pair[0], Q), ("the tensor beside K", pair[1], K)):
-            if like is None:
-                assert t is None, "no K, so no tensor beside it"
-            else:
-                _check_tokens(name, t, like, like.shape[1])
-    views = [tuple(None if t is None else _view(t) for t in pair) for pair in ((Q, K),) + tuple(inputs) + (outputs,)]
+    for pair in (outputs,) if beside is None else (beside, outputs):
+        assert K is not None or pair[1] is None, "no K, so no tensor beside it"
+        views.append((_checked_view("the tensor beside Q", pair[0], Q, shape),
+                      None if K is None else _checked_view("the tensor beside K", pair[1], Q, shape_k)))
     return desc, views, outputs
 
 
@@ -690,7 +691,7 @@ def _outputs_like(tensors, stream):
     """Fresh results in the inputs' order of axes, of the stream that the kernels run on."""
     import torch
     if stream is None:
-        return tuple(None if t is None else torch.empty_like(t) for t in tensors)
+        return tuple([None if t is None else torch.empty_like(t) for t in tensors])
     with torch.cuda.stream(stream):
         return tuple(None if t is None else torch.empty_like(t) for t in tensors)
 
@@ -707,16 +708,17 @@ def _check_weights(weights, Q, K):
     for w, t, name in ((wq, Q, "w_q"), (wk, K, "w_k")):
         if w is None:
             continue
-        assert t is not None and w.is_cuda and w.device == Q.device and w.dtype == torch.float32 and w.is_contiguous(), \
+        assert t is not None and w.get_device() == Q.get_device() and w.dtype == torch.float32 and w.is_contiguous(), \
             name + " must be a dense fp32 tensor on Q's device"
-        assert tuple(w.shape) in ((Q.shape[3],), (t.shape[1], Q.shape[3])), name + " must be [d] or [heads, d]"
-        assert per_head in (None, w.dim() == 2), "w_q and w_k: both [d] or both [heads, d]"
-        per_head = w.dim() == 2
+        own = w.dim() == 2
+        assert w.shape == ((t.shape[1], Q.shape[3]) if own else (Q.shape[3],)), name + " must be [d] or [heads, d]"
+        assert per_head is None or per_head == own, "w_q and w_k: both [d] or both [heads, d]"
+        per_head = own
     return wq, wk, bool(per_head)
 
 
 def _rope_args(Q, K, rope, out, stream):
-    desc, views, outs = _rotary_call(Q, K, rope, (), out, stream)
+    desc, views, outs = _rotary_call(Q, K, rope, None, out, stream)
     (q, k), (qo, ko) = views
     return (ctypes.byref(desc), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream_on(stream, Q.device)), outs, (desc, views)
 
@@ -737,7 +739,7 @@ def agent_rope_bwd(dQ_out, dK_out, rope, *, out=None, stream=None):
 
 
 def _qk_norm_args(Q, K, rope, weights, eps, out, stream):
-    desc, views, outs = _rotary_call(Q, K, rope, (), out, stream)
+    desc, views, outs = _rotary_call(Q, K, rope, None, out, stream)
     wq, wk, per_head = _check_weights(weights, Q, K)
     norm = aa_qk_norm(_ptr(wq), _ptr(wk), int(per_head), eps)
     (q, k), (qo, ko) = views
@@ -755,15 +757,13 @@ def agent_qk_norm_fwd(Q, K, rope=None, *, weights=None, eps=1e-6, out=None, stre
 
 def agent_qk_norm_bwd(Q, K, dQ_out, dK_out, rope=None, *, weights=None, eps=1e-6, want_weight_grads=True, out=None,
                       workspace=None, stream=None):
-    """Gradients of agent_qk_norm_fwd: a dict of dq, dk (None without K) and, for the weights present and
-    want_weight_grads, dw_q, dw_k (fp32).  out: (dQ, dK), which may be (Q, K) or (dQ_out, dK_out)."""
-    import torch
-    desc, views, outs = _rotary_call(Q, K, rope, ((dQ_out, dK_out),), out, stream)
+    """Gradients of agent_qk_norm_fwd: a dict of dq, with K dk and, for the weights present and want_weight_grads, dw_q,
+    dw_k (fp32).  out: (dQ, dK), which may be (Q, K) or (dQ_out, dK_out)."""
+    desc, views, outs = _rotary_call(Q, K, rope, (dQ_out, dK_out), out, stream)
     wq, wk, per_head = _check_weights(weights, Q, K)
     norm = aa_qk_norm(_ptr(wq), _ptr(wk), int(per_head), eps)
     dw = _outputs_like((wq, wk) if want_weight_grads else (None, None), stream)
-    need = 0
-    if dw != (None, None):
+    if dw[0] is not None or dw[1] is not None:
         need = int(lib().agent_qk_norm_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(norm)))
         if workspace is None:
             workspace = _alloc_bytes(max(need, 256), stream, Q.device)
@@ -794,7 +794,7 @@ ACTIVATIONS = {"silu": 0, "gelu": 1, "gelu_tanh": 2, "relu": 3, "sigmoid": 4}
 
 def _ffn_rows(what, t, like):
     """A [..., width] tensor whose rows lie one stride apart: that stride (0: dense)."""
-    assert t.is_cuda and t.device == like.device and t.dtype == like.dtype and tuple(t.shape) == tuple(like.shape), \
+    assert t.get_device() == like.get_device() and t.dtype == like.dtype and t.shape == like.shape, \
         what + " must have x's shape, dtype and device"
     if t.is_contiguous():
         return 0
@@ -805,11 +805,11 @@ def _ffn_rows(what, t, like):
 
 def _ffn_call(x, w_gate, w_up, w_down, b_gate, b_up, b_down, activation):
     assert x.is_cuda and x.dim() >= 2 and x.numel() > 0, "x is a device tensor [..., width]"
-    C, F = x.shape[-1], w_gate.shape[0]
+    C, F, device = x.shape[-1], w_gate.shape[0], x.get_device()
     for t, shape, name in ((w_gate, (F, C), "w_gate"), (w_up, (F, C), "w_up"), (w_down, (C, F), "w_down"),
                            (b_gate, (F,), "b_gate"), (b_up, (F,), "b_up"), (b_down, (C,), "b_down")):
-        assert t is None or (t.is_cuda and t.device == x.device and t.dtype == x.dtype and t.is_contiguous() and
-                             tuple(t.shape) == shape), name + " must be a dense tensor of x's dtype and device, shaped %s" % (shape,)
+        assert t is None or (t.get_device() == device and t.dtype == x.dtype and t.is_contiguous() and
+                             t.shape == shape), name + " must be a dense tensor of x's dtype and device, shaped %s" % (shape,)
     assert w_gate is not None and w_up is not None and w_down is not None
     assert activation in ACTIVATIONS, "activation is one of %s" % (tuple(ACTIVATIONS),)
     desc = aa_ffn(x.numel() // C, C, F, _dtype_code(x), ACTIVATIONS[activation], _ffn_rows("x", x, x), 0, 0)
@@ -848,9 +848,9 @@ def agent_gated_ffn_fwd(x, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_do
 def _dense_like(t, stream):
     import torch
     if stream is None:
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
     with torch.cuda.stream(stream):
-        return torch.empty(t.shape, dtype=t.dtype, device=t.device)
+        return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
 def agent_gated_ffn_bwd(x, dy, saved, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu",
