@@ -69,18 +69,23 @@ struct RotaryPlan {
   int tiles, blocks;     // tiles of tokens, blocks along x
 };
 
-// Backward pass: blocks that walk over the tokens (their sums of the weights' gradients are added up by a second kernel).
+// Backward pass: blocks walk over the tiles and leave sums of the weights' gradients, which a second kernel adds up; at most this
+// many for one weight.
 constexpr int kRotarySumBlocks = 1024;
-// Waves that a launch is cut into where it can be: four for each of the 1024 SIMDs.
-constexpr long long kRotaryWaves = 4096;
+// Waves that a launch is cut into where it can be, two for each of the 1024 SIMDs: with four the norm of 12544 tokens of 6 heads
+// takes 10.0 us and not 8.5, with one it is the same.
+constexpr long long kRotaryWaves = 2048;
 
+// Forward: four waves along the heads (two: long clips 115 us and not 110).  Backward, whose waves hold fewer rows: two, and as
+// many tiles a block as leave two blocks to a CU, up to four, since a block's sums cost as much as a tile (16384 tokens, 8
+// heads each of 64 channels: 25.5 us; a tile each: 27.3, four waves along the heads: 30.4; 12544 tokens, 3 heads: 17.1, 19.3, 22.7).
 inline RotaryPlan rotary_plan(const RotaryShape& s, long long rows, int heads_q, int heads_k, bool backward, bool one_head) {
   // one_head (backward): a wave takes one head, whose weights and sums are its own
   RotaryPlan p{};
   p.lanes = s.lanes;
   while (1 << p.shift < s.lanes) ++p.shift;
   const int most = backward ? std::max(heads_q, heads_k) : heads_q + heads_k;
-  p.across = most >= 3 ? 4 : most;
+  p.across = backward ? std::min(most, 2) : most >= 3 ? 4 : most;
   const long long per = (4 / p.across) * (64 / s.lanes);
   p.tiles = (int)((rows + per - 1) / per);
   auto count = [&](int chunk, int heads) { return (heads + p.across * chunk - 1) / (p.across * chunk); };
@@ -89,8 +94,11 @@ inline RotaryPlan rotary_plan(const RotaryShape& s, long long rows, int heads_q,
   while (p.chunk > 1 && 4 * (long long)p.tiles * blocks(p.chunk) < kRotaryWaves) p.chunk = (p.chunk + 1) / 2;
   p.chunks[0] = count(p.chunk, backward ? heads_q : most), p.chunks[1] = backward ? count(p.chunk, heads_k) : 0;
   p.blocks = p.tiles;
-  if (backward)
-    p.blocks = std::min(p.tiles, std::max(1, kRotarySumBlocks / (one_head ? 1 : std::max(p.chunks[0], p.chunks[1]))));
+  if (backward) {
+    const long long each = std::min(4ll, std::max(1ll, ((long long)p.tiles * blocks(p.chunk) + 256) / 512));
+    const int most_blocks = std::max(1, kRotarySumBlocks / (one_head ? 1 : std::max(p.chunks[0], p.chunks[1])));
+    p.blocks = (int)std::min<long long>((p.tiles + each - 1) / each, most_blocks);
+  }
   return p;
 }
 

@@ -189,7 +189,7 @@ def test_launches_cover_every_row(rules):
                 for backward, one_head in ((0, 0), (1, 0), (1, 1)):
                     shift, across, chunk, cq, ck, tiles, blocks = plan(rows, *heads, lanes, backward, one_head)
                     tokens = 4 // across * (64 // lanes)
-                    assert 1 << shift == lanes and across in (1, 2, 4) and chunk >= 1 and (chunk == 1 or not one_head)
+                    assert 1 << shift == lanes and across in ((1, 2) if backward else (1, 2, 4)) and chunk >= 1 and (chunk == 1 or not one_head)
                     assert (tiles - 1) * tokens < rows <= tiles * tokens and 1 <= blocks <= tiles
                     share = across * chunk
                     for c, n in ((cq, heads[0]), (ck, heads[1])) if backward else ((cq, sum(heads)), (ck, 0)):
