@@ -374,7 +374,7 @@ aa_status agent_qk_norm_bwd(const aa_rotary *desc, const aa_qk_norm *norm, const
  * [width] or NULL; everything in `dtype`.  Sums are fp32; h is rounded to dtype between the products, results are
  * rounded once.  Rows of x, y, dy and dx may be apart (strides in elements, 0: dense).  Tensors of any alignment
  * and width are taken; those whose rows are no whole 16-byte pieces are copied to the workspace first.
- * width, hidden <= 2^20, rows * max(width, hidden) < 2^40. */
+ * width, hidden <= 2^20, rows <= 2^30, rows * max(width, hidden) < 2^40. */
 typedef enum { AA_SILU = 0, AA_GELU = 1, AA_GELU_TANH = 2, AA_RELU = 3, AA_SIGMOID = 4 } aa_activation;
 typedef struct {
   int32_t rows, width, hidden;

@@ -6,7 +6,7 @@
 namespace {
 
 constexpr size_t kAlign = 256;
-constexpr int kMaxWidth = 1 << 20;
+constexpr int kMaxWidth = 1 << 20, kMaxRows = 1 << 30;
 
 aa_status check_ffn(const aa_ffn* d) {
   if (!d) return AA_ERR_NULL;
@@ -17,7 +17,7 @@ aa_status check_ffn(const aa_ffn* d) {
     if (s != 0 && s < d->width) return AA_ERR_SHAPE;
     if (s > 2 * kMaxWidth) return AA_ERR_UNSUPPORTED;
   }
-  if (d->width > kMaxWidth || d->hidden > kMaxWidth) return AA_ERR_UNSUPPORTED;
+  if (d->width > kMaxWidth || d->hidden > kMaxWidth || d->rows > kMaxRows) return AA_ERR_UNSUPPORTED;
   if ((int64_t)d->rows * (d->width > d->hidden ? d->width : d->hidden) >= (int64_t)1 << 40) return AA_ERR_UNSUPPORTED;
   return AA_OK;
 }

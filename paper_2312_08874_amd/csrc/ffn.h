@@ -109,34 +109,36 @@ struct FfnBlock {
 //
 // Microseconds, measured over 4 to 36 steps (16-bit elements, k-contiguous operands; m-contiguous ones within 8 %): a step of as
 // many blocks as a compute unit holds, of one alone, and what a block costs beside its steps.  fp32 steps are those of its matrix
-// rate.
-inline FfnTile ffn_tile(long long M, long long N, long long M2, long long N2, int steps, int es, bool split, bool gated, int compute_units) {
+// rate.  narrow: 64 x 96 tiles may be taken (fp32, results stored as they are), which leave nothing of the widths of three times a
+// power of two unused.
+inline FfnTile ffn_tile(long long M, long long N, long long M2, long long N2, long long steps, int es, bool split, bool gated, int compute_units,
+                        bool narrow = false) {
   struct Shape {
     int rows, cols, held;
     double step, alone, fixed, fixed_alone;
   };
   static const Shape half[4] = {{256, 256, 1, 1.38, 1.38, 9.0, 9.0}, {256, 128, 1, 0.78, 0.78, 5.0, 5.0}, {128, 128, 2, 0.84, 0.56, 6.0, 3.5}, {64, 64, 4, 0.74, 0.35, 3.5, 1.5}};
-  static const Shape single[2] = {{128, 128, 2, 3.75, 2.05, 8.0, 5.0}, {64, 64, 4, 2.0, 0.62, 4.5, 2.0}};
-  FfnTile best{64, 64, 1, 1, steps};
+  static const Shape single[3] = {{128, 128, 2, 3.75, 2.05, 8.0, 5.0}, {64, 64, 4, 2.0, 0.62, 4.5, 2.0}, {64, 96, 3, 2.2, 0.85, 4.5, 2.0}};
+  FfnTile best{64, 64, 1, 1, (int)steps};
   double least = 1e30;
-  for (int i = 0; i < (es == 4 ? 2 : 4); ++i) {
+  for (int i = 0; i < (es == 4 ? (narrow ? 3 : 2) : 4); ++i) {
     const Shape& s = es == 4 ? single[i] : half[i];
     const long long cols = gated ? s.cols / 2 : s.cols;
     const long long tiles = (M + s.rows - 1) / s.rows * ((N + cols - 1) / cols) + (M2 + s.rows - 1) / s.rows * ((N2 + cols - 1) / cols);
     const long long room = (long long)compute_units * s.held;
     // of `blocks` blocks of `each` steps, dealt out evenly
-    auto time = [&](long long blocks, int each) {
+    auto time = [&](long long blocks, long long each) {
       const long long per = (blocks + compute_units - 1) / compute_units, whole = per / s.held, rest = per % s.held;
       const double share = s.held > 1 ? (double)(rest - 1) / (s.held - 1) : 0.0;
       double t = whole * (each * s.step + s.fixed);
       if (rest > 0) t += each * (s.alone + share * (s.step - s.alone)) + s.fixed_alone + share * (s.fixed - s.fixed_alone);
       return t;
     };
-    auto consider = [&](long long full, int parts, int each) {
+    auto consider = [&](long long full, int parts, long long each) {
       double t = time(full, steps);
       if (parts > 1)      // their sums are written, read and added up by one more launch
         t += time((tiles - full) * parts, each) + 4.0 + 8.0e-6 * (tiles - full) * parts * s.rows * s.cols / 4.5;
-      if (t < least) least = t, best = FfnTile{s.rows, s.cols, (int)full, parts, each};
+      if (t < least) least = t, best = FfnTile{s.rows, s.cols, (int)full, parts, (int)each};
     };
     consider(tiles, 1, steps);
     if (!split) continue;
@@ -144,9 +146,10 @@ inline FfnTile ffn_tile(long long M, long long N, long long M2, long long N2, in
     if (tail == 0) continue;
     int before = 1;
     for (int rounds = 1; rounds <= 3; ++rounds) {      // as many parts as fill one, two or three rounds
-      const int most = (int)std::min<long long>(std::min(64, steps / 2), room * rounds / tail);
+      const int most = (int)std::min<long long>(std::min(64ll, steps / 2), room * rounds / tail);
       if (most <= before) continue;
-      const int each = (steps + most - 1) / most, parts = (steps + each - 1) / each;      // every part has steps of its own
+      const long long each = (steps + most - 1) / most;
+      const int parts = (int)((steps + each - 1) / each);      // every part has steps of its own
       if (parts > before) consider(full, parts, each), before = parts;
     }
   }

@@ -82,43 +82,73 @@ __global__ __launch_bounds__(256) void ffn_sum_kernel(FfnGroup g, int rows, int 
   }
 }
 
-// partial[part][c] = sum over the part's rows of in[row][c]: a block takes 64 columns, four rows at a time.
+// Sums over the rows, up to three tensors in one launch: partial[part][first + c] = sum over the part's rows of in[row][c].  A block
+// takes 64 columns, a thread 16 bytes of a row (rows are whole pieces, zeros behind the columns), 32 or 16 rows side by side.
+struct SumJob {
+  const void* in;
+  long long ld;
+  int cols, first;      // columns, and their place in the partial sums, a multiple of 64
+  void* out;
+};
+struct SumJobs {
+  SumJob job[3];
+  int count, rows, rows_each, pitch;
+};
+__device__ __forceinline__ SumJob sum_job(const SumJobs& jobs, int column) {
+  SumJob j = jobs.job[0];
+#pragma unroll
+  for (int i = 1; i < 3; ++i)
+    if (i < jobs.count && column >= jobs.job[i].first) j = jobs.job[i];
+  return j;
+}
 template <class E>
-__global__ __launch_bounds__(256) void ffn_column_sum_kernel(const void* in, long long ld, int rows, int cols, int rows_each, int pitch,
-                                                             float* partial) {
-  __shared__ float sums[4][64];
-  const int c = blockIdx.x * 64 + (threadIdx.x & 63), sub = threadIdx.x >> 6;
-  const int r0 = blockIdx.y * rows_each, r1 = min(rows, r0 + rows_each);
-  float v = 0.0f;
-  if (c < cols) {
-    const typename E::T* p = (const typename E::T*)in + c;
-#pragma unroll 8
-    for (int r = r0 + sub; r < r1; r += 4) v += E::to_f32(p[r * ld]);
+__global__ __launch_bounds__(256) void ffn_column_sum_kernel(SumJobs jobs, float* partial) {
+  using T = typename E::T;
+  constexpr int W = 16 / (int)sizeof(T), kAcross = 64 / W, kSide = 256 / kAcross;
+  __shared__ float sums[kSide][64 + 4];      // + 4: rows on other banks
+  const SumJob j = sum_job(jobs, blockIdx.x * 64);
+  const int at = threadIdx.x % kAcross * W, side = threadIdx.x / kAcross, c = blockIdx.x * 64 - j.first + at;
+  const long long r0 = (long long)blockIdx.y * jobs.rows_each, r1 = min((long long)jobs.rows, r0 + jobs.rows_each);
+  float v[W] = {};
+  if (c < j.cols) {
+    const T* p = (const T*)j.in + c;
+#pragma unroll 4
+    for (long long r = r0 + side; r < r1; r += kSide) {
+      T x[W];
+      const u32x4 raw = *reinterpret_cast<const u32x4*>(p + r * j.ld);
+      __builtin_memcpy(x, &raw, 16);
+#pragma unroll
+      for (int i = 0; i < W; ++i) v[i] += E::to_f32(x[i]);
+    }
   }
-  sums[sub][threadIdx.x & 63] = v;
+#pragma unroll
+  for (int i = 0; i < W; ++i) sums[side][at + i] = v[i];
   __syncthreads();
-  if (sub == 0 && c < cols) {
-    const int i = threadIdx.x;
-    partial[(size_t)blockIdx.y * pitch + c] = (sums[0][i] + sums[1][i]) + (sums[2][i] + sums[3][i]);
-  }
+  if (threadIdx.x >= 64) return;
+  float s[4] = {};
+#pragma unroll
+  for (int i = 0; i < kSide; ++i) s[i & 3] += sums[i][threadIdx.x];
+  partial[(size_t)blockIdx.y * jobs.pitch + blockIdx.x * 64 + threadIdx.x] = (s[0] + s[1]) + (s[2] + s[3]);
 }
 // out[c] = sum over the parts of partial[part][c], in their order, rounded once
 template <class E>
-__global__ __launch_bounds__(256) void ffn_column_total_kernel(const float* partial, int parts, int cols, int pitch, void* out) {
-  const int c = blockIdx.x * 256 + threadIdx.x;
-  if (c >= cols) return;
+__global__ __launch_bounds__(256) void ffn_column_total_kernel(SumJobs jobs, const float* partial, int parts) {
+  const int column = blockIdx.x * 256 + threadIdx.x;
+  if (column >= jobs.pitch) return;
+  const SumJob j = sum_job(jobs, column);
+  if (column - j.first >= j.cols) return;
   float v = 0.0f;
 #pragma unroll 8
-  for (int p = 0; p < parts; ++p) v += partial[(size_t)p * pitch + c];
-  ((typename E::T*)out)[c] = to_elem<E>(v);
+  for (int p = 0; p < parts; ++p) v += partial[(size_t)p * jobs.pitch + column];
+  ((typename E::T*)j.out)[column - j.first] = to_elem<E>(v);
 }
-constexpr int kSumRows = 512;      // rows of a part, at least; at most 64 parts
-int column_parts(int rows) { return std::min(64, (rows + kSumRows - 1) / kSumRows); }
+constexpr int kSumRows = 256;      // rows of a part, at least; at most 64 parts
+int column_parts(int rows) { return (int)std::min(64ll, (rows + (long long)kSumRows - 1) / kSumRows); }
 
 // --- workspaces ---
-int steps_of(const FfnBlock& b, int k) { return (k * b.es() + 127) / 128; }
-FfnTile tile_for(const FfnBlock& b, long long M, long long N, long long M2, long long N2, int k, bool split, bool gated) {
-  return ffn_tile(M, N, M2, N2, steps_of(b, k), b.es(), split, gated, kComputeUnits);
+// stored: the results are, as they are
+FfnTile tile_for(const FfnBlock& b, long long M, long long N, long long M2, long long N2, long long k, bool split, bool gated, bool stored) {
+  return ffn_tile(M, N, M2, N2, (k * b.es() + 127) / 128, b.es(), split, gated, kComputeUnits, stored);
 }
 int tiles_of(const FfnTile& t, long long M, long long N) { return (int)((M + t.rows - 1) / t.rows * ((N + t.cols - 1) / t.cols)); }
 size_t partial_bytes(const FfnTile& t, int tiles) { return t.parts > 1 ? (size_t)(tiles - t.full) * t.parts * t.rows * t.cols * 4 : 0; }
@@ -151,7 +181,7 @@ ForwardPlan forward_plan(const FfnBlock& b) {
     w.total = r.at;
     return w;
   }
-  w.gate = tile_for(b, b.T, pitch, 0, 0, b.C, false, true), w.down = tile_for(b, b.T, b.C, 0, 0, b.F, true, false);
+  w.gate = tile_for(b, b.T, pitch, 0, 0, b.C, false, true, false), w.down = tile_for(b, b.T, b.C, 0, 0, b.F, true, false, true);
   w.x = r.take((size_t)b.T * C * es);
   w.w_gate = r.take((size_t)b.F * C * es), w.w_up = r.take((size_t)b.F * C * es), w.w_down = r.take((size_t)b.C * F * es);
   w.h = r.take((size_t)b.T * pitch * es);
@@ -164,14 +194,14 @@ BackwardPlan backward_plan(const FfnBlock& b) {
   const size_t es = b.es(), pitch = ffn_pitch(b.F), C = round_up(b.C, b.unit()), F = round_up(b.F, b.unit());
   BackwardPlan w;
   Regions r;
-  w.dh = tile_for(b, b.T, pitch, 0, 0, b.C, false, false), w.dx = tile_for(b, b.T, b.C, 0, 0, 2 * pitch, true, false);
-  w.dw = tile_for(b, 2 * pitch, b.C, b.C, b.F, b.T, true, false);
+  w.dh = tile_for(b, b.T, pitch, 0, 0, b.C, false, false, false), w.dx = tile_for(b, b.T, b.C, 0, 0, 2 * pitch, true, false, true);
+  w.dw = tile_for(b, 2 * pitch, b.C, b.C, b.F, b.T, true, false, true);
   w.x = r.take((size_t)b.T * C * es), w.dy = r.take((size_t)b.T * C * es);
   w.w_gate = r.take((size_t)b.F * C * es), w.w_up = r.take((size_t)b.F * C * es), w.w_down = r.take((size_t)b.C * F * es);
   w.dgu = r.take((size_t)b.T * 2 * pitch * es);
   w.partial = r.take(std::max({partial_bytes(w.dx, tiles_of(w.dx, b.T, b.C)),
                                partial_bytes(w.dw, tiles_of(w.dw, 2 * pitch, b.C) + tiles_of(w.dw, b.C, b.F)),
-                               (size_t)column_parts(b.T) * std::max<size_t>(2 * pitch, round_up(b.C, 8)) * 4}));
+                               (size_t)column_parts(b.T) * (2 * pitch + round_up(b.C, 64)) * 4}));
   w.total = r.at;
   return w;
 }
@@ -246,17 +276,19 @@ hipError_t launch_group(const FfnBlock& b, FfnGroup& g, FfnForm form, FfnEpilogu
   return hipGetLastError();
 }
 
-hipError_t column_sums(int dtype, const void* in, long long ld, int rows, int cols, float* partial, void* out, hipStream_t st) {
-  const int parts = column_parts(rows), each = (rows + parts - 1) / parts, pitch = round_up(cols, 8);
-  const dim3 grid((unsigned)((cols + 63) / 64), (unsigned)parts), block(256), total((unsigned)((cols + 255) / 256));
-  if (dtype == 0) ffn_column_sum_kernel<ElemF32><<<grid, block, 0, st>>>(in, ld, rows, cols, each, pitch, partial);
-  else if (dtype == 1) ffn_column_sum_kernel<ElemF16><<<grid, block, 0, st>>>(in, ld, rows, cols, each, pitch, partial);
-  else ffn_column_sum_kernel<ElemBF16><<<grid, block, 0, st>>>(in, ld, rows, cols, each, pitch, partial);
+hipError_t column_sums(int dtype, SumJobs& jobs, float* partial, hipStream_t st) {
+  if (jobs.count == 0) return hipSuccess;
+  const int parts = column_parts(jobs.rows);
+  jobs.rows_each = (int)((jobs.rows + (long long)parts - 1) / parts);
+  const dim3 grid((unsigned)(jobs.pitch / 64), (unsigned)parts), block(256), total((unsigned)((jobs.pitch + 255) / 256));
+  if (dtype == 0) ffn_column_sum_kernel<ElemF32><<<grid, block, 0, st>>>(jobs, partial);
+  else if (dtype == 1) ffn_column_sum_kernel<ElemF16><<<grid, block, 0, st>>>(jobs, partial);
+  else ffn_column_sum_kernel<ElemBF16><<<grid, block, 0, st>>>(jobs, partial);
   const hipError_t err = hipGetLastError();
   if (err != hipSuccess) return err;
-  if (dtype == 0) ffn_column_total_kernel<ElemF32><<<total, block, 0, st>>>(partial, parts, cols, pitch, out);
-  else if (dtype == 1) ffn_column_total_kernel<ElemF16><<<total, block, 0, st>>>(partial, parts, cols, pitch, out);
-  else ffn_column_total_kernel<ElemBF16><<<total, block, 0, st>>>(partial, parts, cols, pitch, out);
+  if (dtype == 0) ffn_column_total_kernel<ElemF32><<<total, block, 0, st>>>(jobs, partial, parts);
+  else if (dtype == 1) ffn_column_total_kernel<ElemF16><<<total, block, 0, st>>>(jobs, partial, parts);
+  else ffn_column_total_kernel<ElemBF16><<<total, block, 0, st>>>(jobs, partial, parts);
   return hipGetLastError();
 }
 
@@ -388,12 +420,20 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
     e.M = b.dw_down ? b.C : 0, e.N = b.F, e.K = b.T, e.out[0] = b.dw_down, e.ldo = b.F;
     FfnTile t = w.dw;
     if (!dw_in || !b.dw_down)      // one of them alone: its own tiles, no more than the plan has room for
-      t = tile_for(b, e.M > 0 ? e.M : d.M, e.M > 0 ? e.N : d.N, 0, 0, b.T, false, false);
+      t = tile_for(b, e.M > 0 ? e.M : d.M, e.M > 0 ? e.N : d.N, 0, 0, b.T, false, false, true);
     AA_TRY(launch_group(b, group, FfnForm::kMM, FfnEpilogue::kStore, t, partial, st));
   }
-  if (b.db_gate) AA_TRY(column_sums(b.dtype, dgu, 2 * (long long)pitch, b.T, b.F, partial, b.db_gate, st));
-  if (b.db_up) AA_TRY(column_sums(b.dtype, (const char*)dgu + (size_t)pitch * b.es(), 2 * (long long)pitch, b.T, b.F, partial, b.db_up, st));
-  if (b.db_down) AA_TRY(column_sums(b.dtype, dy.p, dy.ld, b.T, b.C, partial, b.db_down, st));
+  SumJobs sums{};
+  sums.rows = b.T;
+  auto sum = [&](const void* in, long long ld, int cols, void* out) {
+    if (!out) return;
+    sums.job[sums.count++] = SumJob{in, ld, cols, sums.pitch, out};
+    sums.pitch += round_up(cols, 64);
+  };
+  sum(dgu, 2 * (long long)pitch, b.F, b.db_gate);
+  sum((const char*)dgu + (size_t)pitch * b.es(), 2 * (long long)pitch, b.F, b.db_up);
+  sum(dy.p, dy.ld, b.C, b.db_down);
+  AA_TRY(column_sums(b.dtype, sums, partial, st));
   return hipSuccess;
 }
 
