@@ -48,6 +48,14 @@ def test_cases_reach_the_tiles(rule):
     assert all(t[1] != 96 for shape in SHAPES for t in rule(*shape, narrow=0))
 
 
+def test_most_rows():
+    from paper_2312_08874_amd import binding
+    for rows, taken in ((1 << 30, True), ((1 << 30) + 1, False), ((1 << 31) - 1, False)):
+        for query in (binding.lib().agent_gated_ffn_workspace_bytes, binding.lib().agent_gated_ffn_bwd_workspace_bytes,
+                      binding.lib().agent_gated_ffn_saved_bytes):
+            assert (query(ctypes.byref(binding.aa_ffn(rows, 1, 1, 0, 0, 0, 0, 0))) > 0) == taken
+
+
 @pytest.mark.gpu
 @pytest.mark.parametrize("shape", SHAPES, ids=["x".join(map(str, s)) for s in SHAPES])
 def test_block_and_its_gradients(shape):
