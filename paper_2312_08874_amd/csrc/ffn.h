@@ -16,7 +16,7 @@ inline int ffn_pitch(int hidden) { return (hidden + kFfnPad - 1) / kFfnPad * kFf
 enum class FfnEpilogue {
   kStore,        // out[m][n] = sum (+ bias[n]), rounded to the element type; rows from row_part on go to out[1]
   kGate,         // n is hidden: h = act(gate) up, and what the backward pass needs of it
-  kGateGrad,     // n is hidden: sum = dh; dgate = dh p, dup = dh q
+  kGateGrad,     // n is hidden: sum = dh; dgate = dh p, dup = dh q, side by side in out[0]
 };
 
 // One product D[m][n] = sum over k of A(m,k) B(n,k).  An operand lies k-contiguous ([m][k], leading dimension in elements) or
@@ -29,6 +29,7 @@ struct FfnProduct {
   int a_m, b_m;          // columns of an m-contiguous operand, whole pieces of 16 bytes
   int k_part, b_rows;    // b_parts == 2: a multiple of kFfnPad; rows of an m-contiguous B (of each part), zeros behind them
   int b_parts;
+  int terms;             // kGateGrad: of 2, the second lie behind the first in a row; b_parts == 2: A's k runs through B once for each
   int grid_m, grid_n;
   // epilogues
   void* out[2];
@@ -81,11 +82,15 @@ inline bool ffn_few_rows(int T, int C, int F) {
   // these and those: 512 x 1365, 64 tokens 18.9 and 21.7 us; 1024 x 2816, 32: 17.7, 20.2, 48: 24.8, 20.5; 2048 x 5504, 24: 33.8, 29.3)
   return T <= 16 || (T <= kFfnFewRows && (long long)T * C * F <= 100000000ll);
 }
+// Terms of dgate and dup (16-bit elements), as operands of dx and of the biases' gradients: of few tokens and in small blocks two, as
+// of h in the forward pass of few tokens.  Their products wait for memory and launches (bf16, 64 tokens, 2048 x 5504: 114 us a training
+// step either way), and dx has too few values for the errors of rounded operands to even out.
+inline int ffn_terms(int T, int C, int F, int es) { return es == 2 && (T <= kFfnFewRows || (long long)T * C * F <= 100000000ll) ? 2 : 1; }
 struct FfnRows {
   const void *w[2], *x, *bias[2];
   long long ldx, ldy;
   int M, N, K, pitch, activation;      // pitch: of h and of what is kept
-  void *h, *kept_h, *y;                // h: 16 bits (up to four tokens: two terms, [2][M][pitch]) or fp32; kept_h, p and q for the backward pass, where p_hi is set
+  void *h, *kept_h, *y;                // h: two terms of 16 bits, [2][M][pitch], or fp32; kept_h, p and q for the backward pass, where p_hi is set
   uint16_t *p_hi, *q_hi;
   uint8_t *p_lo, *q_lo;
 };

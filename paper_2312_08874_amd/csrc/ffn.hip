@@ -88,6 +88,7 @@ struct SumJob {
   const void* in;
   long long ld;
   int cols, first;      // columns, and their place in the partial sums, a multiple of 64
+  int second;           // elements to their second term, 0: they have one
   void* out;
 };
 struct SumJobs {
@@ -119,6 +120,12 @@ __global__ __launch_bounds__(256) void ffn_column_sum_kernel(SumJobs jobs, float
       __builtin_memcpy(x, &raw, 16);
 #pragma unroll
       for (int i = 0; i < W; ++i) v[i] += E::to_f32(x[i]);
+      if (j.second > 0) {
+        const u32x4 rest = *reinterpret_cast<const u32x4*>(p + r * j.ld + j.second);
+        __builtin_memcpy(x, &rest, 16);
+#pragma unroll
+        for (int i = 0; i < W; ++i) v[i] += E::to_f32(x[i]);
+      }
     }
   }
 #pragma unroll
@@ -194,11 +201,11 @@ BackwardPlan backward_plan(const FfnBlock& b) {
   const size_t es = b.es(), pitch = ffn_pitch(b.F), C = round_up(b.C, b.unit()), F = round_up(b.F, b.unit());
   BackwardPlan w;
   Regions r;
-  w.dh = tile_for(b, b.T, pitch, 0, 0, b.C, false, false, false), w.dx = tile_for(b, b.T, b.C, 0, 0, 2 * pitch, true, false, true);
+  w.dh = tile_for(b, b.T, pitch, 0, 0, b.C, false, false, false), w.dx = tile_for(b, b.T, b.C, 0, 0, 2 * pitch * ffn_terms(b.T, b.C, b.F, b.es()), true, false, true);
   w.dw = tile_for(b, 2 * pitch, b.C, b.C, b.F, b.T, true, false, true);
   w.x = r.take((size_t)b.T * C * es), w.dy = r.take((size_t)b.T * C * es);
   w.w_gate = r.take((size_t)b.F * C * es), w.w_up = r.take((size_t)b.F * C * es), w.w_down = r.take((size_t)b.C * F * es);
-  w.dgu = r.take((size_t)b.T * 2 * pitch * es);
+  w.dgu = r.take((size_t)b.T * 2 * pitch * es * ffn_terms(b.T, b.C, b.F, b.es()));
   w.partial = r.take(std::max({partial_bytes(w.dx, tiles_of(w.dx, b.T, b.C)),
                                partial_bytes(w.dw, tiles_of(w.dw, 2 * pitch, b.C) + tiles_of(w.dw, b.C, b.F)),
                                (size_t)column_parts(b.T) * (2 * pitch + round_up(b.C, 64)) * 4}));
@@ -375,7 +382,8 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
   *room = bytes >= w.total;
   if (!*room) return hipSuccess;
   const Saved s = saved_plan(b);
-  const int pitch = ffn_pitch(b.F), unit = b.unit(), C = round_up(b.C, unit), F = round_up(b.F, unit);
+  const int pitch = ffn_pitch(b.F), unit = b.unit(), C = round_up(b.C, unit), F = round_up(b.F, unit), terms = ffn_terms(b.T, b.C, b.F, b.es());
+  const long long ldg = 2ll * pitch * terms;      // rows of dgate | dup (| their second terms)
   const char* keep = (const char*)saved;
   float* partial = (float*)(ws + w.partial);
   void* dgu = ws + w.dgu;
@@ -399,7 +407,7 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
     FfnGroup group{};
     FfnProduct& g = group.p[0];
     g.a = dy.p, g.lda = dy.ld, g.b[0] = wd.p, g.ldb = wd.ld, g.b_m = F, g.b_rows = b.C, g.M = b.T, g.N = b.F, g.K = C;
-    g.pitch = pitch, g.hidden = b.F, g.out[0] = dgu;
+    g.pitch = pitch, g.hidden = b.F, g.out[0] = dgu, g.ldo = ldg, g.terms = terms;
     g.p_hi = (uint16_t*)(keep + s.p_hi), g.q_hi = (uint16_t*)(keep + s.q_hi);
     g.p_lo = (uint8_t*)(keep + s.p_lo), g.q_lo = (uint8_t*)(keep + s.q_lo);
     AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kGateGrad, w.dh, nullptr, st));
@@ -407,14 +415,14 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
   if (want_dx) {
     FfnGroup group{};
     FfnProduct& d = group.p[0];
-    d.a = dgu, d.lda = 2 * (long long)pitch, d.b[0] = wg.p, d.b[1] = wu.p, d.ldb = wg.ld, d.b_m = C, d.b_rows = b.F, d.b_parts = 2;
-    d.k_part = pitch, d.M = b.T, d.N = b.C, d.K = 2 * pitch, d.out[0] = b.dx, d.ldo = b.lddx;
+    d.a = dgu, d.lda = ldg, d.terms = terms, d.b[0] = wg.p, d.b[1] = wu.p, d.ldb = wg.ld, d.b_m = C, d.b_rows = b.F, d.b_parts = 2;
+    d.k_part = pitch, d.M = b.T, d.N = b.C, d.K = 2 * pitch * terms, d.out[0] = b.dx, d.ldo = b.lddx;
     AA_TRY(launch_group(b, group, FfnForm::kKM, FfnEpilogue::kStore, w.dx, partial, st));
   }
   if (dw_in || b.dw_down) {      // one launch: together they come nearer to whole rounds of the compute units
     FfnGroup group{};
     FfnProduct &d = group.p[0], &e = group.p[1];
-    d.a = dgu, d.lda = 2 * (long long)pitch, d.a_m = 2 * pitch, d.b[0] = x.p, d.ldb = x.ld, d.b_m = C, d.b_rows = b.T;
+    d.a = dgu, d.lda = ldg, d.a_m = 2 * pitch, d.b[0] = x.p, d.ldb = x.ld, d.b_m = C, d.b_rows = b.T;
     d.M = dw_in ? 2 * pitch : 0, d.N = b.C, d.K = b.T, d.row_part = pitch, d.rows = b.F, d.out[0] = b.dw_gate, d.out[1] = b.dw_up, d.ldo = b.C;
     e.a = dy.p, e.lda = dy.ld, e.a_m = C, e.b[0] = keep + s.h, e.ldb = pitch, e.b_m = pitch, e.b_rows = b.T;
     e.M = b.dw_down ? b.C : 0, e.N = b.F, e.K = b.T, e.out[0] = b.dw_down, e.ldo = b.F;
@@ -425,14 +433,15 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
   }
   SumJobs sums{};
   sums.rows = b.T;
-  auto sum = [&](const void* in, long long ld, int cols, void* out) {
+  auto sum = [&](const void* in, long long ld, int cols, int second, void* out) {
     if (!out) return;
-    sums.job[sums.count++] = SumJob{in, ld, cols, sums.pitch, out};
+    sums.job[sums.count++] = SumJob{in, ld, cols, sums.pitch, second, out};
     sums.pitch += round_up(cols, 64);
   };
-  sum(dgu, 2 * (long long)pitch, b.F, b.db_gate);
-  sum((const char*)dgu + (size_t)pitch * b.es(), 2 * (long long)pitch, b.F, b.db_up);
-  sum(dy.p, dy.ld, b.C, b.db_down);
+  const int second = terms == 2 ? 2 * pitch : 0;
+  sum(dgu, ldg, b.F, second, b.db_gate);
+  sum((const char*)dgu + (size_t)pitch * b.es(), ldg, b.F, second, b.db_up);
+  sum(dy.p, dy.ld, b.C, 0, b.db_down);
   AA_TRY(column_sums(b.dtype, sums, partial, st));
   return hipSuccess;
 }

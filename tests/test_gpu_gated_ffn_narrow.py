@@ -1,5 +1,5 @@
-"""Gated feed-forward block in fp32 where its products take 64 x 96 tiles, and the gradients of the biases; bounds as in
-tests/ffn_reference.py."""
+"""Gated feed-forward block in fp32 where its products take 64 x 96 tiles, the gradients of the biases, and few tokens, whose h, dgate
+and dup are two terms; bounds as in tests/ffn_reference.py."""
 import ctypes
 import os
 import subprocess
@@ -85,3 +85,52 @@ def test_gradients_of_the_biases(shape, dtype):
         one = {k: v for k, v in s.items() if not k.startswith("b_") or k == alone}
         want, got = ref.block(one, "silu"), run(binding, one, "silu")
         check(got["d" + alone], want["d" + alone], alone + " alone")
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("dtype", ["bf16", "f16"])
+@pytest.mark.parametrize("shape", [(1, 216, 512), (4, 64, 130), (5, 40, 77), (16, 128, 300), (17, 64, 96), (40, 96, 250), (64, 72, 200), (500, 64, 130)],
+                         ids=lambda s: "x".join(map(str, s)))
+def test_few_tokens_lose_nothing_between_the_products(shape, dtype):
+    """y (up to 64 tokens) and dx: bounds of operands rounded to 2^-15 (two terms of 8 bits or more) instead of the element type."""
+    from paper_2312_08874_amd import binding
+    s = inputs(dtype, *shape, biases=False)
+    got = run(binding, s, "silu")
+    v = {k: t.double() for k, t in s.items()}
+    g, u = v["x"] @ v["w_gate"].t(), v["x"] @ v["w_up"].t()
+    e = torch.sigmoid(g)
+    a, d = g * e, e * (1 + g * (1 - e))
+    T, C, F = shape
+    U, half, fine, low = 2.0 ** -24, torch.finfo(s["x"].dtype).eps / 2, 2.0 ** -15, 2.0 ** -20
+    eg = (C + 4) * U * (v["x"].abs() @ v["w_gate"].abs().t()) + 2.0 ** -19 * (1 + g.abs())
+    eu = (C + 4) * U * (v["x"].abs() @ v["w_up"].abs().t())
+    h, eh = a * u, u.abs() * 1.2 * eg + a.abs() * eu + eg * eu + fine * (a * u).abs() + low
+    y = h @ v["w_down"].t()
+    bound = half * y.abs() + eh @ v["w_down"].abs().t() + (2 * F + 4) * U * (h.abs() @ v["w_down"].abs().t()) + low
+    assert T > 64 or bool(((got["y"].double() - y).abs() <= bound).all())
+    dh = v["dy"] @ v["w_down"]
+    edh = (C + 4) * U * (v["dy"].abs() @ v["w_down"].abs())
+    dg, du = dh * u * d, dh * a
+    edg = dh.abs() * (d.abs() * eu + (u.abs() + eu) * 1.1 * eg) + (u * d).abs() * edh + 2 * fine * dg.abs() + low
+    edu = dh.abs() * 1.2 * eg + a.abs() * edh + 2 * fine * du.abs() + low
+    dx = dg @ v["w_gate"] + du @ v["w_up"]
+    size = dg.abs() @ v["w_gate"].abs() + du.abs() @ v["w_up"].abs()
+    bound = half * dx.abs() + edg @ v["w_gate"].abs() + edu @ v["w_up"].abs() + (4 * F + 4) * U * size + low
+    assert bool(((got["dx"].double() - dx).abs() <= 1.01 * bound).all())      # 1.01: second orders
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("rows", [1, 4, 5, 17, 64])
+def test_few_tokens_with_h_beyond_the_largest_number(rows):
+    """h = 300 * 300 is beyond fp16, its product with 1/2 is not; an infinite h makes an infinite y, and other rows stay as they are."""
+    from paper_2312_08874_amd import binding
+    x = torch.full((rows, 1), 2.0, dtype=torch.float16, device="cuda")
+    x[0] = 300.0
+    one = torch.ones(1, 1, dtype=torch.float16, device="cuda")
+    y = binding.agent_gated_ffn_fwd(x, one, one, 0.5 * one, activation="relu")
+    assert y[0].item() == torch.tensor(45000.0).half().item() and bool((y[1:] == 2.0).all())
+    for dtype in (torch.float16, torch.bfloat16):
+        z = x.to(dtype)
+        z[0] = float("inf")
+        y = binding.agent_gated_ffn_fwd(z, one.to(dtype), one.to(dtype), one.to(dtype), activation="relu")
+        assert y[0].item() == float("inf") and bool((y[1:] == 4.0).all())
