@@ -392,7 +392,7 @@ typedef struct {
   void *dw_gate, *db_gate, *dw_up, *db_up, *dw_down, *db_down;
 } aa_ffn_grads;
 
-/* Bytes of device workspace of either pass, and of what the forward pass keeps for the backward pass (h, and the
+/* Bytes of device workspace of either pass, and of what the forward pass keeps for the backward pass (h rounded to dtype, and the
  * derivatives of h by gate and by up: 8 bytes a hidden channel of a token for 16-bit types, 12 for fp32).  0 for an
  * invalid descriptor. */
 size_t agent_gated_ffn_workspace_bytes(const aa_ffn *desc);
