@@ -406,8 +406,8 @@ aa_status agent_gated_ffn_fwd(const aa_ffn *desc, const void *x, const aa_ffn_we
 /* Backward pass for the gradient dy of y; x and the weights as in the forward pass (the biases are not read):
  *   dh = dy Wd;  dgate = dh * up * act'(gate), dup = dh * act(gate);  dx = dgate Wg + dup Wu;
  *   dWg = dgate^T x, dWu = dup^T x, dWd = dy^T h; biases: sums over the rows of dgate, dup, dy.
- * dgate and dup are rounded to dtype, as operands of the products (of up to 64 tokens and in small
- * blocks, to two terms of it for dx and the biases).  dx NULL: not wanted.  Results overlap nothing. */
+ * dgate and dup are rounded to dtype, as operands of the products (of up to 64 tokens and in small blocks, to two terms of it); one
+ * that is beyond dtype's range makes the gradients that it is part of infinite or NaN (as two terms: right, up to twice the range).  dx NULL: not wanted.  Results overlap nothing. */
 aa_status agent_gated_ffn_bwd(const aa_ffn *desc, const void *x, const aa_ffn_weights *weights, const void *saved,
                               const void *dy, void *workspace, size_t workspace_bytes, void *dx,
                               const aa_ffn_grads *grads, void *hip_stream);

@@ -30,6 +30,7 @@ struct FfnProduct {
   int k_part, b_rows;    // b_parts == 2: a multiple of kFfnPad; rows of an m-contiguous B (of each part), zeros behind them
   int b_parts;
   int terms;             // kGateGrad: of 2, the second lie behind the first in a row; b_parts == 2: A's k runs through B once for each
+  int b_twice;           // 1: two neighbouring values of k share a row of an m-contiguous B (A's rows are the two terms of each)
   int grid_m, grid_n;
   // epilogues
   void* out[2];
@@ -82,9 +83,10 @@ inline bool ffn_few_rows(int T, int C, int F) {
   // these and those: 512 x 1365, 64 tokens 18.9 and 21.7 us; 1024 x 2816, 32: 17.7, 20.2, 48: 24.8, 20.5; 2048 x 5504, 24: 33.8, 29.3)
   return T <= 16 || (T <= kFfnFewRows && (long long)T * C * F <= 100000000ll);
 }
-// Terms of dgate and dup (16-bit elements), as operands of dx and of the biases' gradients: of few tokens and in small blocks two, as
-// of h in the forward pass of few tokens.  Their products wait for memory and launches (bf16, 64 tokens, 2048 x 5504: 114 us a training
-// step either way), and dx has too few values for the errors of rounded operands to even out.
+// Terms of dgate and dup (16-bit elements), as operands of dx, the weights' and the biases' gradients: of few tokens and in small blocks
+// two, as of h in the forward pass of few tokens.  Their products wait for memory and launches (bf16, 64 tokens, 2048 x 5504: 114 us a
+// training step either way), and dx has too few values for the errors of rounded operands to even out.  The first term alone is
+// no rounding: beyond the type's range it is the largest number, and only both are right or infinite.
 inline int ffn_terms(int T, int C, int F, int es) { return es == 2 && (T <= kFfnFewRows || (long long)T * C * F <= 100000000ll) ? 2 : 1; }
 struct FfnRows {
   const void *w[2], *x, *bias[2];

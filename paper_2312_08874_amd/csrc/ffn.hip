@@ -201,11 +201,12 @@ BackwardPlan backward_plan(const FfnBlock& b) {
   const size_t es = b.es(), pitch = ffn_pitch(b.F), C = round_up(b.C, b.unit()), F = round_up(b.F, b.unit());
   BackwardPlan w;
   Regions r;
-  w.dh = tile_for(b, b.T, pitch, 0, 0, b.C, false, false, false), w.dx = tile_for(b, b.T, b.C, 0, 0, 2 * pitch * ffn_terms(b.T, b.C, b.F, b.es()), true, false, true);
-  w.dw = tile_for(b, 2 * pitch, b.C, b.C, b.F, b.T, true, false, true);
+  const int terms = ffn_terms(b.T, b.C, b.F, b.es());
+  w.dh = tile_for(b, b.T, pitch, 0, 0, b.C, false, false, false), w.dx = tile_for(b, b.T, b.C, 0, 0, 2 * pitch * terms, true, false, true);
+  w.dw = tile_for(b, 2 * pitch, b.C, b.C, b.F, (long long)b.T * terms, true, false, true);
   w.x = r.take((size_t)b.T * C * es), w.dy = r.take((size_t)b.T * C * es);
   w.w_gate = r.take((size_t)b.F * C * es), w.w_up = r.take((size_t)b.F * C * es), w.w_down = r.take((size_t)b.C * F * es);
-  w.dgu = r.take((size_t)b.T * 2 * pitch * es * ffn_terms(b.T, b.C, b.F, b.es()));
+  w.dgu = r.take((size_t)b.T * 2 * pitch * es * terms);
   w.partial = r.take(std::max({partial_bytes(w.dx, tiles_of(w.dx, b.T, b.C)),
                                partial_bytes(w.dw, tiles_of(w.dw, 2 * pitch, b.C) + tiles_of(w.dw, b.C, b.F)),
                                (size_t)column_parts(b.T) * (2 * pitch + round_up(b.C, 64)) * 4}));
@@ -422,13 +423,14 @@ hipError_t launch_ffn_bwd(const FfnBlock& b, const void* saved, void* workspace,
   if (dw_in || b.dw_down) {      // one launch: together they come nearer to whole rounds of the compute units
     FfnGroup group{};
     FfnProduct &d = group.p[0], &e = group.p[1];
-    d.a = dgu, d.lda = ldg, d.a_m = 2 * pitch, d.b[0] = x.p, d.ldb = x.ld, d.b_m = C, d.b_rows = b.T;
-    d.M = dw_in ? 2 * pitch : 0, d.N = b.C, d.K = b.T, d.row_part = pitch, d.rows = b.F, d.out[0] = b.dw_gate, d.out[1] = b.dw_up, d.ldo = b.C;
+    // dgate | dup of a token and their second terms are rows of their own here, both over the token's row of x
+    d.a = dgu, d.lda = 2 * pitch, d.a_m = 2 * pitch, d.b[0] = x.p, d.ldb = x.ld, d.b_m = C, d.b_rows = b.T, d.b_twice = terms - 1;
+    d.M = dw_in ? 2 * pitch : 0, d.N = b.C, d.K = b.T * terms, d.row_part = pitch, d.rows = b.F, d.out[0] = b.dw_gate, d.out[1] = b.dw_up, d.ldo = b.C;
     e.a = dy.p, e.lda = dy.ld, e.a_m = C, e.b[0] = keep + s.h, e.ldb = pitch, e.b_m = pitch, e.b_rows = b.T;
     e.M = b.dw_down ? b.C : 0, e.N = b.F, e.K = b.T, e.out[0] = b.dw_down, e.ldo = b.F;
     FfnTile t = w.dw;
     if (!dw_in || !b.dw_down)      // one of them alone: its own tiles, no more than the plan has room for
-      t = tile_for(b, e.M > 0 ? e.M : d.M, e.M > 0 ? e.N : d.N, 0, 0, b.T, false, false, true);
+      t = tile_for(b, e.M > 0 ? e.M : d.M, e.M > 0 ? e.N : d.N, 0, 0, e.M > 0 ? e.K : d.K, false, false, true);
     AA_TRY(launch_group(b, group, FfnForm::kMM, FfnEpilogue::kStore, t, partial, st));
   }
   SumJobs sums{};

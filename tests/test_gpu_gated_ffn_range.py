@@ -38,3 +38,69 @@ def test_gradient_of_down_where_h_is_beyond_the_largest_number(rows):
     assert not bool(finite[:, 5].any()) and bool(finite[:, :5].all()) and bool(finite[:, 6:].all())
     for name in ("y", "dx", "dw_gate", "dw_up"):
         right(got[name], want[name], name)
+
+
+@pytest.mark.parametrize("rows", ROWS + [300])
+@pytest.mark.parametrize("big", ["dgate", "dup"])
+def test_gradients_where_dgate_or_dup_is_beyond_the_largest_number(big, rows):
+    """One token's dgate or dup of channel 5 is some 70000 to 130000: two terms of fp16 hold it, and its products with x of 1/64 are
+    well inside the range, so that every gradient is right."""
+    from paper_2312_08874_amd import binding
+    s = inputs("f16", rows, 8, 24, False)
+    s["x"] = ((1.0 + s["x"].abs().clamp(max=1.0)) / 64).half()
+    s["dy"] = 0.01 * s["dy"]
+    s["dy"][0] = 25.0
+    s["w_down"][:, 5] = 1.0
+    large, small = ("w_up", "w_gate") if big == "dgate" else ("w_gate", "w_up")
+    s[large][5], s[small][5] = 2500.0, 0.05
+    want, got = ref.block(s, "relu"), run(binding, s, "relu")
+    dh = s["dy"].double() @ s["w_down"].double()
+    factor = (s["x"].double() @ s[large].double().t())[0, 5]
+    assert 66000 < float(dh[0, 5] * factor) < 130000
+    for name in got:
+        assert bool(right(got[name], want[name], name).all()), name
+
+
+@pytest.mark.parametrize("rows", ROWS + [300])
+def test_gradients_with_two_terms_of_dgate_and_dup(rows):
+    """dw_gate and dw_up: dgate and dup in two terms are off by 2^-22 (fp16: 2 x 11 bits), not by 2^-11; an odd number of tokens, and
+    widths that end inside a tile."""
+    from paper_2312_08874_amd import binding
+    s = inputs("f16", rows, 72, 90, False)
+    got = run(binding, s, "sigmoid")
+    v = {k: t.double() for k, t in s.items()}
+    g, u = v["x"] @ v["w_gate"].t(), v["x"] @ v["w_up"].t()
+    U, T, C = 2.0 ** -24, rows, 72
+    eg, eu = ((C + 4) * U * (v["x"].abs() @ v[w].abs().t()) for w in ("w_gate", "w_up"))
+    e = torch.sigmoid(g)
+    ee = 0.25 * eg + 2.0 ** -19 * (1 + g.abs())      # of act and of its derivative, whose slopes are below 1 / 4
+    dh, edh = v["dy"] @ v["w_down"], (C + 4) * U * (v["dy"].abs() @ v["w_down"].abs())
+    p, q = u * e * (1 - e), e
+    ep, eq = (e * (1 - e)) * eu + (u.abs() + eu) * ee + 2.0 ** -16 * p.abs(), ee + 2.0 ** -16 * q
+    for name, f, ef in (("dw_gate", p, ep), ("dw_up", q, eq)):
+        d = dh * f
+        ed = dh.abs() * ef + (f.abs() + ef) * edh + (2.0 ** -21 + U) * d.abs() + 2.0 ** -25      # the last: a subnormal second term
+        want = d.t() @ v["x"]
+        bound = ed.t() @ v["x"].abs() + (2 * T + 4) * U * (d.abs().t() @ v["x"].abs()) + 2.0 ** -11 * want.abs() + 2.0 ** -25
+        off = (got[name].double() - want).abs() - 1.01 * bound      # 1.01: second orders
+        assert bool((off <= 0).all()), "%s: off by %.3g more than allowed" % (name, off.max())
+
+
+@pytest.mark.parametrize("dtype", ["f16", "bf16"])
+@pytest.mark.parametrize("rows", ROWS + [300])
+def test_an_infinite_gradient_of_y_reaches_the_weights_gradients(rows, dtype):
+    """dy of one token is infinite in channel 3: its dgate and dup are infinite, and so is what they or dy make of finite, nonzero x
+    and h; the other channels of dw_down do not meet it."""
+    from paper_2312_08874_amd import binding
+    s = inputs(dtype, rows, 24, 40, True)
+    s["x"] = torch.where(s["x"] == 0, torch.ones_like(s["x"]), s["x"])
+    s["w_down"] = torch.where(s["w_down"] == 0, torch.ones_like(s["w_down"]), s["w_down"])
+    clean = run(binding, s, "silu")
+    s["dy"][rows // 2, 3] = float("inf")
+    got = run(binding, s, "silu")
+    for name in ("dw_gate", "dw_up", "db_gate", "db_up"):
+        assert not bool(torch.isfinite(got[name]).any()), name
+    assert not bool(torch.isfinite(got["dx"][rows // 2]).any())
+    assert not bool(torch.isfinite(got["dw_down"][3]).any()) and not bool(torch.isfinite(got["db_down"][3]).any())
+    others = [c for c in range(24) if c != 3]
+    assert torch.equal(got["dw_down"][others], clean["dw_down"][others])
