@@ -104,3 +104,21 @@ def test_an_infinite_gradient_of_y_reaches_the_weights_gradients(rows, dtype):
     assert not bool(torch.isfinite(got["dw_down"][3]).any()) and not bool(torch.isfinite(got["db_down"][3]).any())
     others = [c for c in range(24) if c != 3]
     assert torch.equal(got["dw_down"][others], clean["dw_down"][others])
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("kind", ["relu", "sigmoid"])
+@pytest.mark.parametrize("rows", [1, 17, 300, 3000])
+def test_gates_of_minus_infinity_switch_their_channels_off(rows, kind, dtype):
+    """As a bias of -10000 does, bit for bit: act and its derivative are 0 at both."""
+    from paper_2312_08874_amd import binding
+    s = inputs(dtype, rows, 40, 200, True)
+    s["b_gate"][::3] = -10000.0
+    want = run(binding, s, kind)
+    s["b_gate"][::3] = float("-inf")
+    got = run(binding, s, kind)
+    for name in want:
+        assert bool(torch.isfinite(want[name]).all()) and torch.equal(got[name], want[name]), name
+    assert not bool(got["dw_gate"][::3].any()) and not bool(got["dw_down"][:, ::3].any())
+    s["x"][0, 0] = float("nan")      # and no number stays none
+    assert bool(run(binding, s, kind)["y"][0].isnan().all())
