@@ -122,3 +122,17 @@ def test_gates_of_minus_infinity_switch_their_channels_off(rows, kind, dtype):
     assert not bool(got["dw_gate"][::3].any()) and not bool(got["dw_down"][:, ::3].any())
     s["x"][0, 0] = float("nan")      # and no number stays none
     assert bool(run(binding, s, kind)["y"][0].isnan().all())
+
+
+@pytest.mark.parametrize("dtype,far", [("bf16", 1e4), ("bf16", 1e20), ("f16", 1e4), ("f32", 1e4), ("f32", 1e20)])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("rows", [1, 17, 300])
+def test_far_gates_are_those_of_relu(rows, kind, dtype, far):
+    """At +-10000 and at +-1e20, whose square is beyond fp32, the activations and their slopes are relu's to the last bit."""
+    from paper_2312_08874_amd import binding
+    s = inputs(dtype, rows, 40, 200, True)
+    s["b_gate"] = torch.where(s["b_gate"] > 0, far, -far).to(s["x"].dtype)
+    s["w_down"] = (s["w_down"].double() / far * 100).to(s["x"].dtype)
+    want, got = run(binding, s, "relu"), run(binding, s, kind)
+    for name in want:
+        assert not bool(want[name].isnan().any()) and torch.equal(got[name], want[name]), name      # dw_down may be beyond fp16
