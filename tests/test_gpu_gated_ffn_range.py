@@ -1,5 +1,7 @@
 """The gated feed-forward block where a value between its products, an input or a gate leaves the element type's range: a result
 is within its bound (tests/ffn_reference.py) or no finite number, and never a finite number that is wrong."""
+import math
+
 import pytest
 import torch
 
@@ -136,3 +138,43 @@ def test_far_gates_are_those_of_relu(rows, kind, dtype, far):
     want, got = run(binding, s, "relu"), run(binding, s, kind)
     for name in want:
         assert not bool(want[name].isnan().any()) and torch.equal(got[name], want[name]), name      # dw_down may be beyond fp16
+
+
+def _tails(kind, g):
+    """act(g) / g, act(g) and its slope without a difference of numbers near 1, which 1 + erf and 1 + tanh are far out."""
+    if kind == "gelu":
+        e = 0.5 * torch.special.erfc(-g * 0.5 ** 0.5)
+        return e, g * e, e + g * torch.exp(-0.5 * g * g) * (2 * math.pi) ** -0.5
+    c = 2 * (2 / math.pi) ** 0.5
+    z, slope = (g, 1.0) if kind == "silu" else (c * (g + 0.044715 * g ** 3), c * (1 + 3 * 0.044715 * g * g))
+    e, rest = torch.sigmoid(z), torch.sigmoid(-z)
+    return e, g * e, e + g * e * rest * slope
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("rows", [16, 64, 241, 30001])
+def test_tails_of_the_activations(rows, kind, dtype):
+    """One hidden channel, whose gate is x's first channel and whose up is large: y is act(g) up and dx its slope times up, so that an
+    error of act shows against act itself.  Bounds, relative: exp of |z| <= 42 with the roundings of its argument and of z,
+    4 * 42 * 2^-24; the fit, 1 / x and what follows, 2^-18; h or dgate, and the result, rounded once each; what the forward pass
+    keeps, 2^-16.  The slope of a negative gate is a difference: relative to the sum of its parts."""
+    from paper_2312_08874_amd import binding
+    up = {"f16": 2.0 ** 14, "bf16": 1.0, "f32": 1.0}[dtype]
+    x = torch.ones(rows, 2, device="cuda")
+    x[:, 0] = torch.linspace(-9, 3, rows)
+    x = x.to(torch.float32 if dtype == "f32" else HALF[dtype])
+
+    def matrix(*v):
+        return torch.tensor(v, device="cuda").to(x.dtype)
+    s = {"x": x, "w_gate": matrix([1.0, 0.0]), "w_up": matrix([0.0, up]), "w_down": matrix([1.0], [0.0]),
+         "dy": matrix([1.0, 0.0]).expand(rows, 2).contiguous()}
+    got = run(binding, s, kind)
+    g = x[:, 0].double()
+    parts, a, d = _tails(kind, g)
+    rest = (d - parts).abs()
+    half, low = torch.finfo(x.dtype).eps / 2, torch.finfo(x.dtype).smallest_normal * torch.finfo(x.dtype).eps
+    near = 4 * 42 * 2.0 ** -24 + 2.0 ** -18
+    assert bool(((got["y"][:, 0].double() - a * up).abs() <= (near + 2.01 * half) * (a * up).abs() + low).all())
+    bound = (near + 2.0 ** -16) * (parts + rest) * up + 2.01 * half * (d * up).abs() + low
+    assert bool(((got["dx"][:, 0].double() - d * up).abs() <= bound).all())
