@@ -151,18 +151,13 @@ def _tails(kind, g):
     return e, g * e, e + g * e * rest * slope
 
 
-@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
-@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
-@pytest.mark.parametrize("rows", [16, 64, 241, 30001])
-def test_tails_of_the_activations(rows, kind, dtype):
-    """One hidden channel, whose gate is x's first channel and whose up is large: y is act(g) up and dx its slope times up, so that an
-    error of act shows against act itself.  Bounds, relative: exp of |z| <= 42 with the roundings of its argument and of z,
-    4 * 42 * 2^-24; the fit, 1 / x and what follows, 2^-18; h or dgate, and the result, rounded once each; what the forward pass
-    keeps, 2^-16.  The slope of a negative gate is a difference: relative to the sum of its parts."""
+def one_channel(rows, kind, dtype, lo, hi):
+    """One hidden channel, whose gate is x's first channel and whose up is large: (gates, up, act(gates) up, its slopes times up, and
+    the type's half rounding and smallest step)."""
     from paper_2312_08874_amd import binding
     up = {"f16": 2.0 ** 14, "bf16": 1.0, "f32": 1.0}[dtype]
     x = torch.ones(rows, 2, device="cuda")
-    x[:, 0] = torch.linspace(-9, 3, rows)
+    x[:, 0] = torch.linspace(lo, hi, rows)
     x = x.to(torch.float32 if dtype == "f32" else HALF[dtype])
 
     def matrix(*v):
@@ -170,11 +165,32 @@ def test_tails_of_the_activations(rows, kind, dtype):
     s = {"x": x, "w_gate": matrix([1.0, 0.0]), "w_up": matrix([0.0, up]), "w_down": matrix([1.0], [0.0]),
          "dy": matrix([1.0, 0.0]).expand(rows, 2).contiguous()}
     got = run(binding, s, kind)
-    g = x[:, 0].double()
+    info = torch.finfo(x.dtype)
+    return x[:, 0].double(), up, got["y"][:, 0].double(), got["dx"][:, 0].double(), info.eps / 2, info.smallest_normal * info.eps
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("kind", ["silu", "gelu", "gelu_tanh"])
+@pytest.mark.parametrize("rows", [16, 64, 241, 30001])
+def test_tails_of_the_activations(rows, kind, dtype):
+    """An error of act shows against act itself.  Bounds, relative: exp of |z| <= 42 with the roundings of its argument and of z,
+    4 * 42 * 2^-24; the fit, 1 / x and what follows, 2^-18; h or dgate, and the result, rounded once each; what the forward pass
+    keeps, 2^-16.  The slope of a negative gate is a difference: relative to the sum of its parts."""
+    g, up, y, dx, half, low = one_channel(rows, kind, dtype, -9, 3)
     parts, a, d = _tails(kind, g)
     rest = (d - parts).abs()
-    half, low = torch.finfo(x.dtype).eps / 2, torch.finfo(x.dtype).smallest_normal * torch.finfo(x.dtype).eps
     near = 4 * 42 * 2.0 ** -24 + 2.0 ** -18
-    assert bool(((got["y"][:, 0].double() - a * up).abs() <= (near + 2.01 * half) * (a * up).abs() + low).all())
+    assert bool(((y - a * up).abs() <= (near + 2.01 * half) * (a * up).abs() + low).all())
     bound = (near + 2.0 ** -16) * (parts + rest) * up + 2.01 * half * (d * up).abs() + low
-    assert bool(((got["dx"][:, 0].double() - d * up).abs() <= bound).all())
+    assert bool(((dx - d * up).abs() <= bound).all())
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("rows", [16, 64, 241, 30001])
+def test_slope_of_the_sigmoid_on_both_sides(rows, dtype):
+    """Up to 13, where it is 2e-6.  Bounds as above, with exp of |z| <= 13."""
+    g, up, y, dx, half, low = one_channel(rows, "sigmoid", dtype, -13, 13)
+    e, rest = torch.sigmoid(g), torch.sigmoid(-g)
+    near = 4 * 13 * 2.0 ** -24 + 2.0 ** -18
+    assert bool(((y - e * up).abs() <= (near + 2.01 * half) * e * up + low).all())
+    assert bool(((dx - e * rest * up).abs() <= (near + 2.0 ** -16 + 2.01 * half) * e * rest * up + low).all())
