@@ -8,6 +8,7 @@ entry point raises.
 from __future__ import annotations
 
 import ctypes
+import functools
 import os
 
 _HERE = os.path.dirname(os.path.abspath(__file__))
@@ -242,10 +243,35 @@ def _check(status, where):
         raise AgentAttnError(status, where)
 
 
+_torch = None
+
+
+def _on_its_device(entry):
+    """An entry point with the device of its first argument current, a tensor or a dict of them: the library launches on the
+    current device, whose null stream the handle 0 is too."""
+    name = entry.__code__.co_varnames[0]
+
+    @functools.wraps(entry)
+    def call(*args, **kw):
+        global _torch
+        if _torch is None:      # an import statement in every call costs as much as all the rest here
+            import torch as _torch
+        t = args[0] if args else kw.get(name)
+        if isinstance(t, dict):
+            t = next((v for v in t.values() if v is not None), None)
+        device = -1 if t is None else t.get_device()
+        if device < 0 or device == _torch._C._cuda_getDevice():
+            return entry(*args, **kw)
+        with _torch.cuda.device(device):
+            return entry(*args, **kw)
+    return call
+
+
 def workspace_bytes(desc: aa_desc, params: aa_params | None = None) -> int:
     return int(lib().agent_attn_workspace_bytes(ctypes.byref(desc), _pp(params)))
 
 
+@_on_its_device
 def agent_attn_bias_tables(params: dict, *, heads, N, n, d, dtype, grid, out=None, stream=None):
     """Agent-bias tables for problems of this shape (dtype: torch dtype of Q), built once from the bias
     components in `params`; returns a uint8 device tensor to pass on as params['bias_tables'], or None
@@ -332,6 +358,7 @@ def _check_agents(A, Q, n, what="A", dtype=None):
         A.shape[3] == Q.shape[3], what + " must be a dense [B,H,n,d] tensor"
 
 
+@_on_its_device
 def agent_attn_fwd(Q, K, V, A=None, *, grid=None, agent_grid=None, params: dict | None = None, scale1=0.0,
                    scale2=0.0, v_residual_k=0.0, n_splits=0, window=None, out=None, workspace=None, stream=None):
     """O = agent attention of Q, K, V [B,H,N,d] (device tensors).  A None: pool Q onto agent_grid.
@@ -354,6 +381,7 @@ def agent_attn_fwd(Q, K, V, A=None, *, grid=None, agent_grid=None, params: dict 
     return out
 
 
+@_on_its_device
 def agent_attn_fwd_static(Q, K, V, A=None, *, grid=None, agent_grid=None, params: dict | None = None, scale1=0.0,
                           scale2=0.0, v_residual_k=0.0, n_splits=0, window=None, out, stream=None):
     """agent_attn_fwd on the library's own static workspace: allocates nothing (`out` is the caller's)."""
@@ -368,6 +396,7 @@ def agent_attn_fwd_static(Q, K, V, A=None, *, grid=None, agent_grid=None, params
     return out
 
 
+@_on_its_device
 def agent_attn_fwd_timed(Q, K, V, A=None, *, grid=None, agent_grid=None, params: dict | None = None, scale1=0.0,
                          scale2=0.0, v_residual_k=0.0, n_splits=0, window=None, out, workspace, stream=None):
     """agent_attn_fwd with each kernel launch timed by HIP events on the launch stream; blocks until the
@@ -386,6 +415,7 @@ def agent_attn_fwd_timed(Q, K, V, A=None, *, grid=None, agent_grid=None, params:
     return [(times[i].name.decode(), float(times[i].ms)) for i in range(count.value)]
 
 
+@_on_its_device
 def agent_attn_resize_bias(params: dict, *, heads, grid, agent_grid, new_agent_grid, stream=None) -> dict:
     """Bias components of `params` adapted to new_agent_grid (Appendix D.1 / D.2); returns a new dict in which
     they are replaced by freshly allocated tensors and every other entry (DWC) is passed through."""
@@ -411,6 +441,7 @@ def agent_attn_resize_bias(params: dict, *, heads, grid, agent_grid, new_agent_g
     return out
 
 
+@_on_its_device
 def agent_attn_module_fwd(x, w_qkv, b_qkv, w_out, b_out, *, heads, grid, agent_grid, window=None,
                           params: dict | None = None, scale1=0.0, scale2=0.0, v_residual_k=0.0, n_splits=0, out=None,
                           workspace=None, stream=None):
@@ -450,6 +481,7 @@ def static_scratch_bytes() -> int:
     return int(lib().agent_attn_static_scratch_bytes())
 
 
+@_on_its_device
 def agent_attn_bwd(Q, K, V, dO, A=None, *, grid=None, agent_grid=None, params: dict | None = None, scale1=0.0,
                    scale2=0.0, v_residual_k=0.0, want_param_grads=True, window=None, workspace=None, stream=None):
     """Gradients of agent_attn_fwd for upstream dO.  Returns a dict: dQ, dK, dV (shape and type of Q),
@@ -495,14 +527,22 @@ class PreparedCall:
     """
 
     def __init__(self, fn, name, args, keep):
+        import torch
         self._fn, self._name, self._args, self._keep = fn, name, args, keep
+        self._device, self._current = torch.cuda.current_device(), torch._C._cuda_getDevice
 
     def __call__(self):
-        st = self._fn(*self._args)
+        if self._current() == self._device:
+            st = self._fn(*self._args)
+        else:
+            import torch
+            with torch.cuda.device(self._device):
+                st = self._fn(*self._args)
         if st != AA_OK:
             raise AgentAttnError(st, self._name)
 
 
+@_on_its_device
 def prepare_fwd(Q, K, V, A=None, *, grid=None, agent_grid=None, params: dict | None = None, scale1=0.0,
                 scale2=0.0, v_residual_k=0.0, n_splits=0, out, workspace=None, stream=None) -> PreparedCall:
     n = A.shape[2] if A is not None else agent_grid[0] * agent_grid[1]
@@ -515,6 +555,7 @@ def prepare_fwd(Q, K, V, A=None, *, grid=None, agent_grid=None, params: dict | N
     return PreparedCall(lib().agent_attn_fwd, "agent_attn_fwd", args, (desc, p, Q, K, V, A, params, workspace, out))
 
 
+@_on_its_device
 def prepare_pool(Q, *, grid, agent_grid, out, stream=None) -> PreparedCall:
     n = agent_grid[0] * agent_grid[1]
     desc = _desc_from(Q, n, grid, agent_grid)
@@ -522,6 +563,7 @@ def prepare_pool(Q, *, grid, agent_grid, out, stream=None) -> PreparedCall:
     return PreparedCall(lib().agent_pool_fwd, "agent_pool_fwd", args, (desc, Q, out))
 
 
+@_on_its_device
 def prepare_aggregate(A, K, V, *, grid=None, params: dict | None = None, scale1=0.0, n_splits=0, out,
                       workspace=None, stream=None) -> PreparedCall:
     desc = _desc_from(K, A.shape[2], grid, None, same=(V,), scale1=scale1, n_splits=n_splits)
@@ -533,6 +575,7 @@ def prepare_aggregate(A, K, V, *, grid=None, params: dict | None = None, scale1=
                         (desc, p, A, K, V, params, workspace, out))
 
 
+@_on_its_device
 def prepare_broadcast(Q, A, VA, V=None, *, grid=None, params: dict | None = None, scale2=0.0, v_residual_k=0.0,
                       out, stream=None) -> PreparedCall:
     desc = _desc_from(Q, A.shape[2], grid, None, same=(V,), out=out, scale2=scale2, v_residual_k=v_residual_k)
@@ -542,6 +585,7 @@ def prepare_broadcast(Q, A, VA, V=None, *, grid=None, params: dict | None = None
     return PreparedCall(lib().agent_broadcast_fwd, "agent_broadcast_fwd", args, (desc, p, Q, A, VA, V, params, out))
 
 
+@_on_its_device
 def agent_pool_fwd(Q, *, grid, agent_grid, out=None, stream=None):
     import torch
     B, H, N, d = Q.shape
@@ -555,6 +599,7 @@ def agent_pool_fwd(Q, *, grid, agent_grid, out=None, stream=None):
     return out
 
 
+@_on_its_device
 def agent_aggregate_fwd(A, K, V, *, grid=None, params: dict | None = None, scale1=0.0, n_splits=0, out=None,
                         workspace=None, stream=None):
     import torch
@@ -574,6 +619,7 @@ def agent_aggregate_fwd(A, K, V, *, grid=None, params: dict | None = None, scale
     return out
 
 
+@_on_its_device
 def agent_broadcast_fwd(Q, A, VA, V=None, *, grid=None, params: dict | None = None, scale2=0.0,
                         v_residual_k=0.0, out=None, stream=None):
     import torch
@@ -591,7 +637,7 @@ def agent_broadcast_fwd(Q, A, VA, V=None, *, grid=None, params: dict | None = No
 
 
 def _stream_on(stream, device):
-    """The stream's handle, or that of the current stream of the tensors' device."""
+    """The stream's handle, or that of the current stream of the tensors' device (which is current: _on_its_device)."""
     import torch
     return torch._C._cuda_getCurrentRawStream(device.index) if stream is None else stream.cuda_stream
 
@@ -723,6 +769,7 @@ def _rope_args(Q, K, rope, out, stream):
     return (ctypes.byref(desc), _ref(q), _ref(k), _ref(qo), _ref(ko), _stream_on(stream, Q.device)), outs, (desc, views)
 
 
+@_on_its_device
 def agent_rope_fwd(Q, K, rope, *, out=None, stream=None):
     """Queries Q [B,H,N,d] and keys K [B,H',N,d] (or None) rotated by their positions; any strides, channels side by side.
     out: (Q', K'), which may be (Q, K) themselves.  Returns (Q', K')."""
@@ -731,6 +778,7 @@ def agent_rope_fwd(Q, K, rope, *, out=None, stream=None):
     return outs
 
 
+@_on_its_device
 def agent_rope_bwd(dQ_out, dK_out, rope, *, out=None, stream=None):
     """Gradients of agent_rope_fwd for the gradients of its results: (dQ, dK)."""
     args, outs, keep = _rope_args(dQ_out, dK_out, rope, out, stream)
@@ -747,6 +795,7 @@ def _qk_norm_args(Q, K, rope, weights, eps, out, stream):
         (desc, norm, views)
 
 
+@_on_its_device
 def agent_qk_norm_fwd(Q, K, rope=None, *, weights=None, eps=1e-6, out=None, stream=None):
     """Every row of Q and K divided by its root mean square, times its weights, then rotated (rope None: not), in one
     pass.  weights: (w_q, w_k), fp32, both [d] or both [heads, d]; None: ones.  Tensors as for agent_rope_fwd."""
@@ -755,6 +804,7 @@ def agent_qk_norm_fwd(Q, K, rope=None, *, weights=None, eps=1e-6, out=None, stre
     return outs
 
 
+@_on_its_device
 def agent_qk_norm_bwd(Q, K, dQ_out, dK_out, rope=None, *, weights=None, eps=1e-6, want_weight_grads=True, out=None,
                       workspace=None, stream=None):
     """Gradients of agent_qk_norm_fwd: a dict of dq, with K dk and, for the weights present and want_weight_grads, dw_q,
@@ -777,11 +827,13 @@ def agent_qk_norm_bwd(Q, K, dQ_out, dK_out, rope=None, *, weights=None, eps=1e-6
     return {name: t for name, t in grads.items() if t is not None}
 
 
+@_on_its_device
 def prepare_rope(Q, K, rope, *, out, stream=None) -> PreparedCall:
     args, outs, keep = _rope_args(Q, K, rope, out, stream)
     return PreparedCall(lib().agent_rope_fwd, "agent_rope_fwd", args, (keep, Q, K, rope, outs))
 
 
+@_on_its_device
 def prepare_qk_norm(Q, K, rope=None, *, weights=None, eps=1e-6, out, stream=None) -> PreparedCall:
     args, outs, keep = _qk_norm_args(Q, K, rope, weights, eps, out, stream)
     return PreparedCall(lib().agent_qk_norm_fwd, "agent_qk_norm_fwd", args, (keep, Q, K, rope, weights, outs))
@@ -831,6 +883,7 @@ def _ffn_fwd_args(x, w, desc, out, saved, workspace, stream):
             workspace.numel() * workspace.element_size(), out.data_ptr(), _stream_on(stream, x.device)), workspace
 
 
+@_on_its_device
 def agent_gated_ffn_fwd(x, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu", save=False,
                         out=None, workspace=None, stream=None):
     """y = (act(x w_gate^T + b_gate) * (x w_up^T + b_up)) w_down^T + b_down for x [..., width], weights [hidden, width],
@@ -853,6 +906,7 @@ def _dense_like(t, stream):
         return torch.empty_like(t, memory_format=torch.contiguous_format)
 
 
+@_on_its_device
 def agent_gated_ffn_bwd(x, dy, saved, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu",
                         want_dx=True, want_weight_grads=True, workspace=None, stream=None):
     """Gradients of agent_gated_ffn_fwd for the gradient dy of its result; saved: what that call returned.  A dict of dx
@@ -879,6 +933,7 @@ def agent_gated_ffn_bwd(x, dy, saved, w_gate, w_up, w_down, *, b_gate=None, b_up
     return out
 
 
+@_on_its_device
 def prepare_gated_ffn(x, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down=None, activation="silu", out,
                       workspace=None, stream=None) -> PreparedCall:
     desc, w = _ffn_call(x, w_gate, w_up, w_down, b_gate, b_up, b_down, activation)
