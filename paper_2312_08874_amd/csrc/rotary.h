@@ -69,6 +69,12 @@ struct RotaryPlan {
   int tiles, blocks;     // tiles of tokens, blocks along x
 };
 
+// Forward: blocks along x at most, since a launch has to stay below 2^32 threads there (2^26 tokens of 256 channels are 2^24 blocks of
+// 256); more tiles lie along z, this many a layer.  (As launches of their own, which hand the kernel a first tile: 4096 x 2 tokens
+// 8.0 us and not 7.8.)
+constexpr int kRotaryLaunchBlocks = 1 << 23;
+inline int rotary_layers(const RotaryPlan& p) { return (p.blocks - 1) / kRotaryLaunchBlocks + 1; }
+
 // Backward pass: blocks walk over the tiles and leave sums of the weights' gradients, which a second kernel adds up; at most this
 // many for one weight.
 constexpr int kRotarySumBlocks = 1024;
