@@ -76,6 +76,11 @@ AA_HOST_DEVICE void ffn_place(unsigned at, unsigned grid_m, unsigned grid_n, int
 // neighbours, so that its L2 serves what they share.  count or more: no work.
 AA_HOST_DEVICE unsigned ffn_run(unsigned L, unsigned count) { return (L & 7u) * ((count + 7u) / 8u) + (L >> 3); }
 
+// A launch of `blocks` blocks: this many along x at most, since it has to stay below 2^32 threads there (2^30 rows of 16 channels are
+// 2^24 blocks of 256); further ones lie along y, and the last layer may have blocks without work.
+constexpr unsigned kFfnLaunchBlocks = 1u << 22;
+inline unsigned ffn_layers(long long blocks) { return (unsigned)((blocks + kFfnLaunchBlocks - 1) / kFfnLaunchBlocks); }
+
 // A few tokens: x -> h (w: gate and up, K = width, N = hidden) and h -> y (w[0]: down, K = hidden, N = width).  Weights [N][K], dense.
 constexpr int kFfnFewRows = 64;      // most tokens of their kernels
 inline bool ffn_few_rows(int T, int C, int F) {
