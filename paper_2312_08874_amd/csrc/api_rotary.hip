@@ -89,23 +89,26 @@ bool bytes_meet(const void* a, size_t na, const void* b, size_t nb) {
   return x < y + nb && y < x + na;
 }
 
-// Tensors whose extents meet are apart all the same where both repeat with one period (the token's or the sequence's stride)
+// Elements that a tensor takes of every `period`: those along axes whose strides are whole periods lie at the same place of theirs.
+long long part_of(const aa_rotary* r, const Span& s, long long period) {
+  long long extent = r->d;
+  const std::pair<long long, long long> axes[3] = {{s.sb, r->batch}, {s.sh, s.heads}, {s.sn, r->tokens}};
+  for (const auto& a : axes)
+    if (a.first % period != 0) extent += (a.second - 1) * a.first;
+  return extent;
+}
+
+// Tensors whose extents meet are apart all the same where both repeat with one period (a head's, token's or sequence's stride)
 // and take different parts of it, as the slices of a fused projection do.
 bool views_meet(const aa_rotary* r, const Span& a, const Span& b) {
   const long long es = elem_bytes(r);
   if (!bytes_meet(a.view->data, (size_t)(extent_of(r, a) * es), b.view->data, (size_t)(extent_of(r, b) * es))) return false;
   const long long diff = (long long)((intptr_t)b.view->data - (intptr_t)a.view->data);
-  auto apart = [&](long long period, long long wa, long long wb) {
-    if (period <= 0 || wa > period || wb > period) return false;
-    const long long p = period * es, at = (diff % p + p) % p;
-    return at >= wa * es && at + wb * es <= p;
-  };
-  if (a.sn == b.sn && (r->batch == 1 || (a.sn > 0 && a.sb % a.sn == 0 && b.sb % a.sn == 0)) &&
-      apart(a.sn, (a.heads - 1) * a.sh + r->d, (b.heads - 1) * b.sh + r->d))
-    return false;
-  if (a.sb == b.sb && r->batch > 1 &&
-      apart(a.sb, extent_of(r, a) - (r->batch - 1) * a.sb, extent_of(r, b) - (r->batch - 1) * b.sb))
-    return false;
+  for (const long long period : {a.sh, a.sn, a.sb, b.sh, b.sn, b.sb}) {
+    if (period <= 0) continue;
+    const long long wa = part_of(r, a, period), wb = part_of(r, b, period), p = period * es, at = (diff % p + p) % p;
+    if (wa <= period && at >= wa * es && at + wb * es <= p) return false;
+  }
   return true;
 }
 
