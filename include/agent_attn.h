@@ -400,7 +400,8 @@ size_t agent_gated_ffn_saved_bytes(const aa_ffn *desc);
 size_t agent_gated_ffn_bwd_workspace_bytes(const aa_ffn *desc);
 
 /* Forward pass.  saved: NULL, or agent_gated_ffn_saved_bytes() of device memory that the backward pass of these rows
- * reads; saved and workspace 256-byte aligned (AA_ERR_WORKSPACE).  y overlaps nothing. */
+ * reads; saved and workspace 256-byte aligned (AA_ERR_WORKSPACE).  y overlaps nothing (AA_ERR_ALIAS); columns of one buffer, of
+ * equal strides, count as apart.  Strides of rows up to 2^21 elements. */
 aa_status agent_gated_ffn_fwd(const aa_ffn *desc, const void *x, const aa_ffn_weights *weights, void *saved,
                               void *workspace, size_t workspace_bytes, void *y, void *hip_stream);
 /* Backward pass for the gradient dy of y; x and the weights as in the forward pass (the biases are not read):

@@ -34,11 +34,18 @@ aa::FfnBlock block_of(const aa_ffn* d) {
 struct Range {
   const void* p;
   size_t bytes;
+  size_t pitch = 0, row = 0;      // rows of `row` bytes, `pitch` apart; 0: one piece
 };
+Range rows_of(const void* p, long long rows, long long ld, size_t cols, size_t es) {
+  return Range{p, ((size_t)(rows - 1) * ld + cols) * es, (size_t)ld * es, cols * es};
+}
 bool meet(const Range& a, const Range& b) {
   if (!a.p || !b.p) return false;
   const uintptr_t x = (uintptr_t)a.p, y = (uintptr_t)b.p;
-  return x < y + b.bytes && y < x + a.bytes;
+  if (x >= y + b.bytes || y >= x + a.bytes) return false;
+  if (a.pitch == 0 || a.pitch != b.pitch) return true;
+  const size_t at = y >= x ? (y - x) % a.pitch : (a.pitch - (x - y) % a.pitch) % a.pitch;      // columns of one buffer are apart
+  return at < a.row || at + b.row > a.pitch;
 }
 // `results` are written (the workspace among them), `inputs` read: no result may meet another or an input
 template <size_t R, size_t I>
@@ -78,8 +85,8 @@ aa_status agent_gated_ffn_fwd(const aa_ffn* desc, const void* x, const aa_ffn_we
   if (!workspace || ((uintptr_t)workspace % kAlign) != 0) return AA_ERR_WORKSPACE;
   if (((uintptr_t)saved % kAlign) != 0) return AA_ERR_WORKSPACE;
   const size_t es = b.es(), C = b.C, F = b.F, in = C * F * es;
-  const Range results[] = {{y, ((size_t)(b.T - 1) * b.ldy + C) * es}, {workspace, workspace_bytes}, {saved, aa::ffn_saved_bytes(b)}};
-  const Range inputs[] = {{x, ((size_t)(b.T - 1) * b.ldx + C) * es}, {w->w_gate, in}, {w->w_up, in}, {w->w_down, in},
+  const Range results[] = {rows_of(y, b.T, b.ldy, C, es), {workspace, workspace_bytes}, {saved, aa::ffn_saved_bytes(b)}};
+  const Range inputs[] = {rows_of(x, b.T, b.ldx, C, es), {w->w_gate, in}, {w->w_up, in}, {w->w_down, in},
                           {w->b_gate, F * es}, {w->b_up, F * es}, {w->b_down, C * es}};
   const aa_status at = check_ranges(results, inputs, es);
   if (at != AA_OK) return at;
@@ -100,9 +107,9 @@ aa_status agent_gated_ffn_bwd(const aa_ffn* desc, const void* x, const aa_ffn_we
   if (((uintptr_t)saved % kAlign) != 0) return AA_ERR_WORKSPACE;
   const aa_ffn_grads none{}, *to = g ? g : &none;
   const size_t es = b.es(), C = b.C, F = b.F, in = C * F * es;
-  const Range results[] = {{dx, ((size_t)(b.T - 1) * b.lddx + C) * es}, {workspace, workspace_bytes}, {to->dw_gate, in}, {to->dw_up, in},
+  const Range results[] = {rows_of(dx, b.T, b.lddx, C, es), {workspace, workspace_bytes}, {to->dw_gate, in}, {to->dw_up, in},
                            {to->dw_down, in}, {to->db_gate, F * es}, {to->db_up, F * es}, {to->db_down, C * es}};
-  const Range inputs[] = {{x, ((size_t)(b.T - 1) * b.ldx + C) * es}, {dy, ((size_t)(b.T - 1) * b.ldy + C) * es}, {w->w_gate, in},
+  const Range inputs[] = {rows_of(x, b.T, b.ldx, C, es), rows_of(dy, b.T, b.ldy, C, es), {w->w_gate, in},
                           {w->w_up, in}, {w->w_down, in}, {saved, aa::ffn_saved_bytes(b)}};
   const aa_status at = check_ranges(results, inputs, es);
   if (at != AA_OK) return at;
