@@ -5,7 +5,7 @@
     z = y + gated feed-forward block of rms(y) w2
 
 Matrix products and the norms over the whole width are torch's; everything between them is one call of the library, and
-torch.autograd.Function ties its backward pass to autograd.
+torch.autograd.Function ties its backward pass to autograd, once: a second derivative through them is an error.
 
     python -m paper_2312_08874_amd.block [--dtype bf16] [--batch 8] [--side 32] [--width 512] [--heads 8] [--steps 20]
 
@@ -16,6 +16,7 @@ import math
 import time
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import binding
 
@@ -37,6 +38,7 @@ class _Attention(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, d_out):
         qkv, w_q, w_k, turned = ctx.saved_tensors
         q, k, _ = (t.permute(0, 2, 1, 3) for t in qkv.unbind(2))
@@ -58,6 +60,7 @@ class _FeedForward(torch.autograd.Function):
         return y
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         x, w_gate, w_up, w_down, saved = ctx.saved_tensors
         g = binding.agent_gated_ffn_bwd(x, dy.contiguous(), saved, w_gate, w_up, w_down, activation=ctx.activation)
