@@ -339,7 +339,7 @@ typedef struct {
 
 /* Queries and keys rotated.  Each result may be its own input (same pointer and strides); otherwise results overlap
  * nothing (AA_ERR_ALIAS), where rows that interleave, as the q / k / v slices of a fused projection do, count as
- * apart.  k and k_out are not read with heads_k == 0.
+ * apart.  k and k_out, w_k and dw_k below, are not read with heads_k == 0.
  * Errors: AA_ERR_NULL, AA_ERR_SHAPE (sizes, pairs, grid, strides), AA_ERR_DTYPE, AA_ERR_UNSUPPORTED (d > 256, 2^31 tokens). */
 aa_status agent_rope_fwd(const aa_rotary *desc, const aa_view *q, const aa_view *k, const aa_view *q_out,
                          const aa_view *k_out, void *hip_stream);

@@ -166,8 +166,13 @@ aa_status make_args(const aa_rotary* r, const aa_view* const in[2], const aa_vie
 aa_status check_norm(const aa_rotary* r, const aa_qk_norm* norm) {
   if (!norm) return AA_ERR_NULL;
   if (!(norm->eps >= 0.0f) || !isfinite(norm->eps)) return AA_ERR_SHAPE;
-  if (((uintptr_t)norm->w_q & 3) || ((uintptr_t)norm->w_k & 3)) return AA_ERR_SHAPE;
+  if (((uintptr_t)norm->w_q & 3) || (r->heads_k > 0 && ((uintptr_t)norm->w_k & 3))) return AA_ERR_SHAPE;
   return AA_OK;
+}
+
+// without keys w_k may be anything: waves without heads would read it
+const float* weight_of(const aa_rotary* r, const aa_qk_norm* norm, int which) {
+  return which == 0 ? norm->w_q : r->heads_k > 0 ? norm->w_k : nullptr;
 }
 
 size_t weight_bytes(const aa_rotary* r, const aa_qk_norm* norm, int which) {
@@ -225,7 +230,7 @@ aa_status agent_qk_norm_fwd(const aa_rotary* desc, const aa_qk_norm* norm, const
   st = make_args(desc, in, nullptr, out, &a, &shape);
   if (st != AA_OK) return st;
   for (int i = 0; i < 2; ++i) {
-    a.weight[i] = i ? norm->w_k : norm->w_q;
+    a.weight[i] = weight_of(desc, norm, i);
     if (results_meet(desc, a, a.weight[i], weight_bytes(desc, norm, i))) return AA_ERR_ALIAS;
   }
   a.weight_heads = norm->per_head != 0, a.eps = norm->eps;
@@ -262,12 +267,12 @@ aa_status agent_qk_norm_bwd(const aa_rotary* desc, const aa_qk_norm* norm, const
   if (results_meet(desc, a, workspace, workspace_bytes)) return AA_ERR_ALIAS;
   for (int i = 0; i < 2; ++i) {
     const size_t bytes = weight_bytes(desc, norm, i);
-    a.weight[i] = i ? norm->w_k : norm->w_q;
+    a.weight[i] = weight_of(desc, norm, i);
     if ((uintptr_t)dw[i] & 3) return AA_ERR_SHAPE;
     if (results_meet(desc, a, a.weight[i], bytes) || results_meet(desc, a, dw[i], bytes)) return AA_ERR_ALIAS;
     if (bytes_meet(workspace, workspace_bytes, a.weight[i], bytes) || bytes_meet(workspace, workspace_bytes, dw[i], bytes)) return AA_ERR_ALIAS;
     for (int j = 0; j < 2; ++j)
-      if (bytes_meet(dw[i], bytes, j ? norm->w_k : norm->w_q, weight_bytes(desc, norm, j))) return AA_ERR_ALIAS;
+      if (bytes_meet(dw[i], bytes, weight_of(desc, norm, j), weight_bytes(desc, norm, j))) return AA_ERR_ALIAS;
     for (int j = 0; j < tensors; ++j)
       for (const aa::TokenView* v : {&a.in[j], &a.grad[j]}) {
         const long long n = (desc->batch - 1) * v->sb + (a.heads[j] - 1) * v->sh + (desc->tokens - 1) * v->sn + desc->d;
