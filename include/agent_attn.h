@@ -372,7 +372,7 @@ aa_status agent_qk_norm_bwd(const aa_rotary *desc, const aa_qk_norm *norm, const
  *   gate = x Wg^T + bg,  up = x Wu^T + bu,  h = act(gate) * up,  y = h Wd^T + bd
  * x, y [rows][width]; Wg, Wu [hidden][width], Wd [width][hidden], all row-major and dense, biases [hidden], [hidden],
  * [width] or NULL; everything in `dtype`.  Sums are fp32; h is rounded to dtype between the products (of a few tokens,
- * to two terms of it), results are rounded once.  Rows of x, y, dy and dx may be apart (strides in elements, 0: dense).  Tensors of any alignment
+ * to two terms of it for y), results are rounded once.  Rows of x, y, dy and dx may be apart (strides in elements, 0: dense).  Tensors of any alignment
  * and width are taken; those whose rows are no whole 16-byte pieces are copied to the workspace first.
  * width, hidden <= 2^20, rows <= 2^30, rows * max(width, hidden) < 2^40. */
 typedef enum { AA_SILU = 0, AA_GELU = 1, AA_GELU_TANH = 2, AA_RELU = 3, AA_SIGMOID = 4 } aa_activation;
@@ -407,8 +407,9 @@ aa_status agent_gated_ffn_fwd(const aa_ffn *desc, const void *x, const aa_ffn_we
 /* Backward pass for the gradient dy of y; x and the weights as in the forward pass (the biases are not read):
  *   dh = dy Wd;  dgate = dh * up * act'(gate), dup = dh * act(gate);  dx = dgate Wg + dup Wu;
  *   dWg = dgate^T x, dWu = dup^T x, dWd = dy^T h; biases: sums over the rows of dgate, dup, dy.
- * dgate and dup are rounded to dtype, as operands of the products (of up to 64 tokens and in small blocks, to two terms of it); one
- * that is beyond dtype's range makes the gradients that it is part of infinite or NaN (as two terms: right, up to twice the range).  dx NULL: not wanted.  Results overlap nothing. */
+ * dgate and dup are rounded to dtype, as operands of the products (of up to 64 tokens and in small blocks, to two terms of it).  One
+ * beyond dtype's range makes the gradients that it is part of infinite or NaN (two terms hold twice the range).  dx NULL: not
+ * wanted.  Results overlap nothing (as above). */
 aa_status agent_gated_ffn_bwd(const aa_ffn *desc, const void *x, const aa_ffn_weights *weights, const void *saved,
                               const void *dy, void *workspace, size_t workspace_bytes, void *dx,
                               const aa_ffn_grads *grads, void *hip_stream);
