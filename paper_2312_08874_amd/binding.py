@@ -258,7 +258,7 @@ def _on_its_device(entry):
             import torch as _torch
         t = args[0] if args else kw.get(name)
         if isinstance(t, dict):
-            t = next((v for v in t.values() if v is not None), None)
+            t = next((v for v in t.values() if isinstance(v, _torch.Tensor)), None)
         device = -1 if t is None else t.get_device()
         if device < 0 or device == _torch._C._cuda_getDevice():
             return entry(*args, **kw)
