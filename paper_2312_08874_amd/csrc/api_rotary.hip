@@ -3,10 +3,8 @@
 
 #include <math.h>
 
-#include <algorithm>
-#include <utility>
-
 #include "kernels.h"
+#include "token_views.h"
 
 namespace {
 
@@ -15,11 +13,8 @@ using aa::RotaryMode;
 
 constexpr size_t kAlign = 256;
 
-struct Span {      // a token tensor with its sizes, in elements
-  const aa_view* view;
-  long long sb, sh, sn;
-  int heads;
-};
+using Span = aa::TokenSpan;
+using aa::bytes_meet;
 
 aa_status check_rotary(const aa_rotary* r) {
   if (!r) return AA_ERR_NULL;
@@ -52,67 +47,11 @@ aa_status check_rotary(const aa_rotary* r) {
 int elem_bytes(const aa_rotary* r) { return r->dtype == AA_F32 ? 4 : 2; }
 
 aa_status check_view(const aa_rotary* r, const aa_view* v, int heads, bool result, Span* out) {
-  if (!v || !v->data) return AA_ERR_NULL;
-  const int es = elem_bytes(r);
-  if ((uintptr_t)v->data % es) return AA_ERR_SHAPE;
-  Span s{v, v->stride_b, v->stride_h, v->stride_n, heads};
-  if (s.sb < 0 || s.sh < 0 || s.sn < 0) return AA_ERR_SHAPE;
-  if (s.sb == 0 && s.sh == 0 && s.sn == 0) {
-    s.sn = r->d, s.sh = (long long)r->tokens * r->d, s.sb = s.sh * heads;
-  }
-  const long long lim = 1ll << 40;
-  if (s.sb > lim || s.sh > lim || s.sn > lim) return AA_ERR_UNSUPPORTED;
-  std::pair<long long, long long> axis[3] = {{s.sb, r->batch}, {s.sh, heads}, {s.sn, r->tokens}};
-  std::sort(axis, axis + 3);
-  long long extent = r->d;
-  for (const auto& a : axis) {
-    if (a.second == 1) continue;
-    if (result && a.first < extent) return AA_ERR_SHAPE;
-    if (a.first > (lim - extent) / a.second) return AA_ERR_UNSUPPORTED;
-    extent += a.first * (a.second - 1);
-  }
-  *out = s;
-  return AA_OK;
+  *out = Span{nullptr, 0, 0, 0, r->batch, heads, r->tokens, r->d, elem_bytes(r)};
+  return aa::check_token_view(v, result, out);
 }
 
-long long extent_of(const aa_rotary* r, const Span& s) {      // elements from the first to behind the last
-  return (r->batch - 1) * s.sb + (s.heads - 1) * s.sh + (r->tokens - 1) * s.sn + r->d;
-}
-
-bool same(const Span& a, const Span& b) {
-  return a.view->data == b.view->data && a.sb == b.sb && a.sh == b.sh && a.sn == b.sn && a.heads == b.heads;
-}
-
-bool bytes_meet(const void* a, size_t na, const void* b, size_t nb) {
-  if (!a || !b || !na || !nb) return false;
-  const uintptr_t x = (uintptr_t)a, y = (uintptr_t)b;
-  return x < y + nb && y < x + na;
-}
-
-// Elements that a tensor takes of every `period`: those along axes whose strides are whole periods lie at the same place of theirs.
-long long part_of(const aa_rotary* r, const Span& s, long long period) {
-  long long extent = r->d;
-  const std::pair<long long, long long> axes[3] = {{s.sb, r->batch}, {s.sh, s.heads}, {s.sn, r->tokens}};
-  for (const auto& a : axes)
-    if (a.first % period != 0) extent += (a.second - 1) * a.first;
-  return extent;
-}
-
-// Tensors whose extents meet are apart all the same where both repeat with one period (a head's, token's or sequence's stride)
-// and take different parts of it, as the slices of a fused projection do.
-bool views_meet(const aa_rotary* r, const Span& a, const Span& b) {
-  const long long es = elem_bytes(r);
-  if (!bytes_meet(a.view->data, (size_t)(extent_of(r, a) * es), b.view->data, (size_t)(extent_of(r, b) * es))) return false;
-  const long long diff = (long long)((intptr_t)b.view->data - (intptr_t)a.view->data);
-  for (const long long period : {a.sh, a.sn, a.sb, b.sh, b.sn, b.sb}) {
-    if (period <= 0) continue;
-    const long long wa = part_of(r, a, period), wb = part_of(r, b, period), p = period * es, at = (diff % p + p) % p;
-    if (wa <= period && at >= wa * es && at + wb * es <= p) return false;
-  }
-  return true;
-}
-
-void place(aa::TokenView* v, const Span& s) { *v = aa::TokenView{(char*)s.view->data, s.sb, s.sh, s.sn}; }
+void place(aa::TokenView* v, const Span& s) { *v = aa::TokenView{s.data, s.sb, s.sh, s.sn}; }
 
 // Validates the views of one call and fills the kernel's arguments; groups: the inputs, the gradients (or null), the results.
 aa_status make_args(const aa_rotary* r, const aa_view* const in[2], const aa_view* const grad[2], const aa_view* const out[2],
@@ -131,7 +70,7 @@ aa_status make_args(const aa_rotary* r, const aa_view* const in[2], const aa_vie
       Span s;
       const aa_status st = check_view(r, group[i], a->heads[i], g == 2, &s);
       if (st != AA_OK) return st;
-      align |= (uintptr_t)s.view->data | (unsigned long long)((s.sb | s.sh | s.sn) * es);
+      align |= (uintptr_t)s.data | (unsigned long long)((s.sb | s.sh | s.sn) * es);
       place(g == 0 ? &a->in[i] : g == 1 ? &a->grad[i] : &a->out[i], s);
       spans[n++] = s;
     }
@@ -140,8 +79,8 @@ aa_status make_args(const aa_rotary* r, const aa_view* const in[2], const aa_vie
   const int results = n - tensors;
   for (int o = results; o < n; ++o)
     for (int i = 0; i < n; ++i) {
-      if (i == o || (i < results && i % tensors == o - results && same(spans[i], spans[o]))) continue;
-      if (views_meet(r, spans[i], spans[o])) return AA_ERR_ALIAS;
+      if (i == o || (i < results && i % tensors == o - results && spans[i].same_place(spans[o]))) continue;
+      if (aa::spans_meet(spans[i], spans[o])) return AA_ERR_ALIAS;
     }
   if (r->axes > 0) {
     for (int x = 0; x < aa::kRotaryAxes; ++x) {
@@ -156,7 +95,7 @@ aa_status make_args(const aa_rotary* r, const aa_view* const in[2], const aa_vie
       a->positions_batch = r->positions_shared ? 0 : (long long)r->tokens * r->axes;
       const size_t bytes = (size_t)4 * r->axes * r->tokens * (r->positions_shared ? 1 : r->batch);
       for (int o = results; o < n; ++o)
-        if (bytes_meet(spans[o].view->data, (size_t)extent_of(r, spans[o]) * es, r->positions, bytes)) return AA_ERR_ALIAS;
+        if (bytes_meet(spans[o].data, spans[o].bytes(), r->positions, bytes)) return AA_ERR_ALIAS;
     }
   }
   *shape = aa::rotary_shape(es, r->d, r->pairing, r->axes, a->first, align);
