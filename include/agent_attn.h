@@ -300,7 +300,7 @@ size_t agent_attn_plan_str(const aa_desc *desc, int agents_given, char *buf, siz
 
 /* ------------------------------------------------------------------------
  * Operators of a transformer block around the attention: rotary positions, norms of queries and keys, the gated
- * feed-forward block.  Conventions as above: device pointers (where not marked as host memory), host-only
+ * feed-forward block, softmax attention, layer norm.  Conventions as above: device pointers (where not marked as host memory), host-only
  * validation before anything is launched, no allocation, no synchronisation, the same bits from the same inputs.
  * ---------------------------------------------------------------------- */
 
@@ -413,6 +413,77 @@ aa_status agent_gated_ffn_fwd(const aa_ffn *desc, const void *x, const aa_ffn_we
 aa_status agent_gated_ffn_bwd(const aa_ffn *desc, const void *x, const aa_ffn_weights *weights, const void *saved,
                               const void *dy, void *workspace, size_t workspace_bytes, void *dx,
                               const aa_ffn_grads *grads, void *hip_stream);
+
+/* Softmax attention of whole sequences: of query row i of head h and the keys and values of head h / (heads_q / heads_k)
+ *   o_i = sum over j of p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i),  lse_i = log(sum over j of exp(scale q_i . k_j)),
+ * j over the keys that the row sees: all of its sequence's, or, causal, those up to i + (keys - queries) (the last query sees
+ * the last key).  A row that sees none: o = 0, lse = -infinity, no gradient.  Host struct:
+ *   whole   sequences 0, lengths NULL: `batch` sequences of tokens_q queries and tokens_k keys
+ *   padded  lengths_q, lengths_k: device, int32, [batch], either may be NULL (every row): rows in use from the first on
+ *   packed  sequences > 0, batch 1: rows starts_q[s] .. starts_q[s+1] - 1 and starts_k[s] .. starts_k[s+1] - 1 (device, int32,
+ *           [sequences + 1], rising, within tokens_q and tokens_k) are sequence s, which may be empty
+ * Rows of no sequence are not used, whatever they hold, and as results stay as they were.  Lengths and starts are read on the
+ * device and kept within the tensors' rows there; starts that fall give results of no meaning.
+ * Scores and sums are fp32; p (and, backward, ds) is rounded to dtype, as an operand; results are rounded once.  A NaN or
+ * infinity in a row of a sequence may show in every result of that head's sequence.  d <= 256. */
+typedef struct {
+  int32_t batch, heads_q, heads_k; /* heads_q a multiple of heads_k */
+  int32_t tokens_q, tokens_k;      /* rows of q, out and of k, v */
+  int32_t d, dtype;                /* channels of a head; aa_dtype of every token tensor */
+  int32_t causal;
+  int32_t sequences;               /* packed: their number; else 0 */
+  const int32_t *starts_q, *starts_k;
+  const int32_t *lengths_q, *lengths_k;
+  float scale;                     /* 0: d^-1/2 */
+} aa_softmax_attn;
+
+/* Bytes of device workspace of either pass, which may be 0 for the forward pass.  Tensors whose rows are no whole, aligned 16-byte
+ * pieces are copied there first; a view that is NULL counts as one of them.  0 for an invalid descriptor. */
+size_t agent_softmax_attn_workspace_bytes(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v);
+size_t agent_softmax_attn_bwd_workspace_bytes(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
+                                              const aa_view *dout);
+/* lse: NULL, or [batch][heads_q][tokens_q] for the backward pass.  Results overlap nothing (slices of one buffer as above).
+ * Errors: AA_ERR_NULL, AA_ERR_SHAPE, AA_ERR_DTYPE, AA_ERR_UNSUPPORTED (d > 256, more blocks or elements than can be numbered),
+ * AA_ERR_WORKSPACE (256-byte aligned), AA_ERR_ALIAS. */
+aa_status agent_softmax_attn_fwd(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
+                                 void *workspace, size_t workspace_bytes, const aa_view *out, float *lse, void *hip_stream);
+/* Gradients for the gradient dout of out, from what the forward pass read and left:
+ *   D_i = dout_i . out_i,  ds_ij = p_ij (dout_i . v_j - D_i),
+ *   dq_i = scale sum over j of ds_ij k_j,  dk_j = scale sum over i of ds_ij q_i,  dv_j = sum over i of p_ij dout_i,
+ * the last two over all query heads that share the keys.  The same inputs give the same bits. */
+aa_status agent_softmax_attn_bwd(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
+                                 const aa_view *out, const float *lse, const aa_view *dout, void *workspace,
+                                 size_t workspace_bytes, const aa_view *dq, const aa_view *dk, const aa_view *dv,
+                                 void *hip_stream);
+
+/* Rows of a tensor [rows][width] in memory: stride in elements (0: dense). */
+typedef struct {
+  void *data;
+  int64_t stride;
+} aa_rows;
+
+/* Layer norm of every row, with the residual sum before it in the same pass (host struct):
+ *   s = x + residual,  h = (s - mean s) r,  r = (mean of (s - mean s)^2 + eps)^-1/2,  y = h weight + bias
+ * Sums are fp32, the mean is taken off before the squares are summed; s is normed unrounded.  weight, bias: device, dense
+ * [width], in fp32 or dtype; NULL: ones, zeros.  width <= 32768.  A row of equal values with eps 0 has no norm (NaN). */
+typedef struct {
+  int32_t rows, width;
+  int32_t dtype, weight_dtype; /* aa_dtype of the rows; of weight and bias: AA_F32 or dtype */
+  float eps;                   /* >= 0 */
+} aa_layer_norm;
+/* residual, sum (s rounded to dtype) and saved may be NULL; saved: [rows][2] floats for the backward pass, the rows' mean and r.
+ * y and sum may be the rows of x or of residual (same pointer and stride) and otherwise overlap nothing (AA_ERR_ALIAS). */
+aa_status agent_layer_norm_fwd(const aa_layer_norm *desc, const aa_rows *x, const aa_rows *residual, const void *weight,
+                               const void *bias, const aa_rows *y, const aa_rows *sum, float *saved, void *hip_stream);
+/* Gradients, from the normed rows x (the sum, where there was a residual) and the gradient dy of y; dsum: NULL, or a gradient of s from
+ * elsewhere, which is added:
+ *   g = dy weight,  dx = r (g - mean g - h mean(g h)) + dsum,  dweight = sum over the rows of dy h,  dbias = sum of dy
+ * dx is the gradient of x and of residual; it may be the rows of x, dy or dsum.  dweight, dbias: in the weight's type; NULL, as dx:
+ * not wanted; summed in a fixed order.  workspace: needed for dweight, dbias alone, 256-byte aligned. */
+size_t agent_layer_norm_bwd_workspace_bytes(const aa_layer_norm *desc);
+aa_status agent_layer_norm_bwd(const aa_layer_norm *desc, const aa_rows *x, const aa_rows *dy, const float *saved,
+                               const void *weight, const aa_rows *dsum, void *workspace, size_t workspace_bytes,
+                               const aa_rows *dx, void *dweight, void *dbias, void *hip_stream);
 
 /* Static string for a status code. */
 const char *agent_attn_status_str(int status);

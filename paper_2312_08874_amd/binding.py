@@ -88,6 +88,21 @@ class aa_ffn_grads(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("dw_gate", "db_gate", "dw_up", "db_up", "dw_down", "db_down")]
 
 
+class aa_softmax_attn(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_int32) for n in ("batch", "heads_q", "heads_k", "tokens_q", "tokens_k", "d", "dtype", "causal",
+                                              "sequences")] + \
+               [(n, ctypes.c_void_p) for n in ("starts_q", "starts_k", "lengths_q", "lengths_k")] + [("scale", ctypes.c_float)]
+
+
+class aa_rows(ctypes.Structure):
+    _fields_ = [("data", ctypes.c_void_p), ("stride", ctypes.c_int64)]
+
+
+class aa_layer_norm(ctypes.Structure):
+    _fields_ = [("rows", ctypes.c_int32), ("width", ctypes.c_int32), ("dtype", ctypes.c_int32),
+                ("weight_dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
+
+
 EXPORTS = ("agent_attn_workspace_bytes", "agent_attn_fwd", "agent_pool_fwd", "agent_aggregate_fwd",
            "agent_broadcast_fwd", "agent_attn_flops", "agent_attn_status_str", "agent_attn_plan_str",
            "agent_attn_bwd_workspace_bytes", "agent_attn_bwd", "agent_attn_bias_tables_bytes",
@@ -95,7 +110,9 @@ EXPORTS = ("agent_attn_workspace_bytes", "agent_attn_fwd", "agent_pool_fwd", "ag
            "agent_attn_fwd_timed", "agent_attn_resize_bias", "agent_attn_module_workspace_bytes",
            "agent_attn_module_fwd", "agent_rope_fwd", "agent_rope_bwd", "agent_qk_norm_fwd", "agent_qk_norm_bwd",
            "agent_qk_norm_bwd_workspace_bytes", "agent_gated_ffn_workspace_bytes", "agent_gated_ffn_saved_bytes",
-           "agent_gated_ffn_bwd_workspace_bytes", "agent_gated_ffn_fwd", "agent_gated_ffn_bwd")
+           "agent_gated_ffn_bwd_workspace_bytes", "agent_gated_ffn_fwd", "agent_gated_ffn_bwd",
+           "agent_softmax_attn_workspace_bytes", "agent_softmax_attn_bwd_workspace_bytes", "agent_softmax_attn_fwd",
+           "agent_softmax_attn_bwd", "agent_layer_norm_fwd", "agent_layer_norm_bwd_workspace_bytes", "agent_layer_norm_bwd")
 
 _lib = None
 
@@ -173,6 +190,22 @@ def lib():
         L.agent_gated_ffn_fwd.argtypes = [fp, vp, wp, vp, vp, ctypes.c_size_t, vp, vp]
         L.agent_gated_ffn_bwd.restype = ctypes.c_int
         L.agent_gated_ffn_bwd.argtypes = [fp, vp, wp, vp, vp, vp, ctypes.c_size_t, vp, gp, vp]
+        sp = ctypes.POINTER(aa_softmax_attn)
+        L.agent_softmax_attn_workspace_bytes.restype = ctypes.c_size_t
+        L.agent_softmax_attn_workspace_bytes.argtypes = [sp, tv, tv, tv]
+        L.agent_softmax_attn_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.agent_softmax_attn_bwd_workspace_bytes.argtypes = [sp, tv, tv, tv, tv]
+        L.agent_softmax_attn_fwd.restype = ctypes.c_int
+        L.agent_softmax_attn_fwd.argtypes = [sp, tv, tv, tv, vp, ctypes.c_size_t, tv, vp, vp]
+        L.agent_softmax_attn_bwd.restype = ctypes.c_int
+        L.agent_softmax_attn_bwd.argtypes = [sp, tv, tv, tv, tv, vp, tv, vp, ctypes.c_size_t, tv, tv, tv, vp]
+        lp, ro = ctypes.POINTER(aa_layer_norm), ctypes.POINTER(aa_rows)
+        L.agent_layer_norm_fwd.restype = ctypes.c_int
+        L.agent_layer_norm_fwd.argtypes = [lp, ro, ro, vp, vp, ro, ro, vp, vp]
+        L.agent_layer_norm_bwd_workspace_bytes.restype = ctypes.c_size_t
+        L.agent_layer_norm_bwd_workspace_bytes.argtypes = [lp]
+        L.agent_layer_norm_bwd.restype = ctypes.c_int
+        L.agent_layer_norm_bwd.argtypes = [lp, ro, ro, vp, vp, ro, vp, ctypes.c_size_t, ro, vp, vp, vp]
         L.agent_attn_status_str.restype = ctypes.c_char_p
         L.agent_attn_status_str.argtypes = [ctypes.c_int]
         _lib = L
@@ -940,3 +973,192 @@ def prepare_gated_ffn(x, w_gate, w_up, w_down, *, b_gate=None, b_up=None, b_down
     args, workspace = _ffn_fwd_args(x, w, desc, out, None, workspace, stream)
     return PreparedCall(lib().agent_gated_ffn_fwd, "agent_gated_ffn_fwd", args,
                         (desc, w, x, w_gate, w_up, w_down, b_gate, b_up, b_down, workspace, out))
+
+
+# --- softmax attention ---
+
+def _ints(what, t, like, count):
+    import torch
+    if t is None:
+        return None
+    assert t.get_device() == like.get_device() and t.dtype == torch.int32 and t.is_contiguous() and t.shape == (count,), \
+        "%s: a dense int32 tensor of %d values on Q's device" % (what, count)
+    return t.data_ptr()
+
+
+def _softmax_call(Q, K, V, causal, starts, lengths, scale):
+    """Descriptor and views of Q, K and V."""
+    assert Q.is_cuda and Q.dim() == 4 and K.dim() == 4, "Q, K and V must be [B,H,N,d] on the GPU"
+    B, H, N, d = Q.shape
+    shape_k = (B, K.shape[1], K.shape[2], d)
+    views = (_view(Q), _checked_view("K", K, Q, shape_k), _checked_view("V", V, Q, shape_k))
+    assert starts is None or lengths is None, "sequences are packed or padded, not both"
+    desc = aa_softmax_attn(B, H, shape_k[1], N, shape_k[2], d, _dtype_code(Q), int(causal), scale=scale)
+    if starts is not None:
+        starts_q, starts_k = starts
+        assert B == 1 and starts_q.dim() == 1 and len(starts_q) > 1, "packed sequences are one batch element's rows"
+        desc.sequences = len(starts_q) - 1
+        desc.starts_q = _ints("starts of the queries", starts_q, Q, len(starts_q))
+        desc.starts_k = _ints("starts of the keys", starts_k, Q, len(starts_q))
+    elif lengths is not None:
+        desc.lengths_q, desc.lengths_k = _ints("lengths of the queries", lengths[0], Q, B), _ints("lengths of the keys", lengths[1], Q, B)
+    return desc, views
+
+
+def _fresh_tokens(t, zeros, stream):
+    """A result like t, in its order of axes where that is dense; zeros where rows of no sequence are left as they are."""
+    import torch
+    make = torch.zeros_like if zeros else torch.empty_like
+    if stream is None:
+        return make(t)
+    with torch.cuda.stream(stream):
+        return make(t)
+
+
+def _softmax_workspace(need, workspace, stream, device):
+    if workspace is None:
+        return _alloc_bytes(need, stream, device) if need else None
+    assert workspace.is_cuda and workspace.is_contiguous() and workspace.device == device
+    return workspace
+
+
+def _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, lse, out, workspace, stream):
+    desc, (q, k, v) = _softmax_call(Q, K, V, causal, starts, lengths, scale)
+    o = _checked_view("out", out, Q, Q.shape)
+    need = int(lib().agent_softmax_attn_workspace_bytes(ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v)))
+    workspace = _softmax_workspace(need, workspace, stream, Q.device)
+    return (ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v), _ptr(workspace),
+            0 if workspace is None else workspace.numel() * workspace.element_size(), ctypes.byref(o), _ptr(lse),
+            _stream_on(stream, Q.device)), (desc, q, k, v, o, workspace)
+
+
+@_on_its_device
+def agent_softmax_attn_fwd(Q, K, V, *, causal=False, starts=None, lengths=None, scale=0.0, save=False, out=None, workspace=None,
+                           stream=None):
+    """Softmax attention of Q [B,H,N,d] over K, V [B,H',M,d], H a multiple of H' (consecutive query heads share keys); any strides,
+    channels side by side.  causal: a query sees the keys up to its place from the end.  lengths: (of the queries, of the
+    keys), int32 [B] on the device, either None: rows in use of every sequence.  starts: (of the queries, of the keys), int32
+    [S+1] on the device: S sequences packed into one batch element's rows.  scale 0: d^-1/2.  save: also returns what
+    agent_softmax_attn_bwd needs, (out, lse).  Rows of no sequence: zeros, or what `out` held."""
+    import torch
+    if out is None:
+        out = _fresh_tokens(Q, starts is not None or lengths is not None, stream)
+    lse = None
+    if save:
+        lse = _alloc_bytes(4 * Q.shape[0] * Q.shape[1] * Q.shape[2], stream, Q.device).view(torch.float32).view(Q.shape[:3])
+    args, keep = _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, lse, out, workspace, stream)
+    _check(lib().agent_softmax_attn_fwd(*args), "agent_softmax_attn_fwd")
+    return (out, lse) if save else out
+
+
+@_on_its_device
+def agent_softmax_attn_bwd(Q, K, V, out, lse, dO, *, causal=False, starts=None, lengths=None, scale=0.0, grads=None, workspace=None,
+                           stream=None):
+    """Gradients of agent_softmax_attn_fwd for the gradient dO of its result `out`; lse: what it returned.  A dict of dQ, dK, dV.
+    grads: (dQ, dK, dV) to write to, whose rows of no sequence stay as they are (fresh ones: zeros)."""
+    import torch
+    desc, (q, k, v) = _softmax_call(Q, K, V, causal, starts, lengths, scale)
+    assert lse.get_device() == Q.get_device() and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == Q.shape[:3], \
+        "lse is what the forward pass returned"
+    o, g = _checked_view("out", out, Q, Q.shape), _checked_view("dO", dO, Q, Q.shape)
+    if grads is None:
+        grads = tuple(_fresh_tokens(t, starts is not None or lengths is not None, stream) for t in (Q, K, V))
+    dq, dk, dv = (_checked_view("d" + n, t, Q, like.shape) for n, t, like in zip("QKV", grads, (Q, K, V)))
+    need = int(lib().agent_softmax_attn_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v),
+                                                            ctypes.byref(g)))
+    workspace = _softmax_workspace(need, workspace, stream, Q.device)
+    st = lib().agent_softmax_attn_bwd(ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v), ctypes.byref(o),
+                                      lse.data_ptr(), ctypes.byref(g), _ptr(workspace),
+                                      0 if workspace is None else workspace.numel() * workspace.element_size(), ctypes.byref(dq),
+                                      ctypes.byref(dk), ctypes.byref(dv), _stream_on(stream, Q.device))
+    _check(st, "agent_softmax_attn_bwd")
+    return dict(zip(("dQ", "dK", "dV"), grads))
+
+
+@_on_its_device
+def prepare_softmax_attn(Q, K, V, *, causal=False, starts=None, lengths=None, scale=0.0, out, workspace=None, stream=None) -> PreparedCall:
+    """The lengths or starts may change on the device between the calls."""
+    args, keep = _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, None, out, workspace, stream)
+    return PreparedCall(lib().agent_softmax_attn_fwd, "agent_softmax_attn_fwd", args, (keep, Q, K, V, starts, lengths, out))
+
+
+# --- layer norm ---
+
+def _norm_rows(what, t, like):
+    return None if t is None else ctypes.byref(aa_rows(t.data_ptr(), _ffn_rows(what, t, like)))
+
+
+def _norm_call(x, weight, bias, eps):
+    assert x.is_cuda and x.dim() >= 1 and x.numel() > 0, "x is a device tensor [..., width]"
+    import torch
+    C, code = x.shape[-1], _dtype_code(x)
+    desc = aa_layer_norm(x.numel() // C, C, code, code, eps)
+    types = set()
+    for t, name in ((weight, "weight"), (bias, "bias")):
+        if t is not None:
+            assert t.get_device() == x.get_device() and t.is_contiguous() and t.shape == (C,) and t.dtype in (torch.float32, x.dtype), \
+                name + " must be a dense [%d] tensor in fp32 or x's dtype, on its device" % C
+            types.add(t.dtype)
+    assert len(types) < 2, "weight and bias have one dtype"
+    if torch.float32 in types:
+        desc.weight_dtype = AA_F32
+    return desc
+
+
+def _layer_norm_args(x, weight, bias, residual, eps, saved, out, sum_out, stream):
+    desc = _norm_call(x, weight, bias, eps)
+    return (ctypes.byref(desc), _norm_rows("x", x, x), _norm_rows("residual", residual, x), _ptr(weight), _ptr(bias),
+            _norm_rows("out", out, x), _norm_rows("sum_out", sum_out, x), _ptr(saved), _stream_on(stream, x.device))
+
+
+@_on_its_device
+def agent_layer_norm_fwd(x, weight=None, bias=None, *, residual=None, eps=1e-5, save=False, out=None, sum_out=None, stream=None):
+    """y = (s - mean s) / sqrt(var s + eps) * weight + bias along the last axis of s = x + residual (None: x).  Tensors are dense, or
+    [rows, width] with rows one stride apart; weight and bias [width] in fp32 or x's dtype.  Returns y, with a residual (y, s), and with
+    save what agent_layer_norm_bwd needs behind them.  out and sum_out (to which s is written) may be x or residual."""
+    import torch
+    if out is None:
+        out = _dense_like(x, stream)
+    if sum_out is None and residual is not None:
+        sum_out = _dense_like(x, stream)
+    saved = None
+    if save:
+        saved = _alloc_bytes(8 * (x.numel() // x.shape[-1]), stream, x.device).view(torch.float32).view(*x.shape[:-1], 2)
+    _check(lib().agent_layer_norm_fwd(*_layer_norm_args(x, weight, bias, residual, eps, saved, out, sum_out, stream)), "agent_layer_norm_fwd")
+    results = (out,) + (() if sum_out is None else (sum_out,)) + ((saved,) if save else ())
+    return results if len(results) > 1 else out
+
+
+@_on_its_device
+def agent_layer_norm_bwd(x, dy, saved, weight=None, bias=None, *, dsum=None, want_dx=True, want_weight_grads=True, out=None,
+                         workspace=None, stream=None):
+    """Gradients of agent_layer_norm_fwd for the gradient dy of its y; x: what was normed (s, with a residual), saved: what the forward
+    pass returned, dsum: a gradient of s from elsewhere, which is added.  A dict of dx (the gradient of x and of residual) and, for
+    the weights present and want_weight_grads, dw and db in their type.  out: dx, which may be x, dy or dsum."""
+    import torch
+    desc = _norm_call(x, weight, bias, 0.0)
+    rows = x.numel() // x.shape[-1]
+    assert saved.get_device() == x.get_device() and saved.dtype == torch.float32 and saved.is_contiguous() and saved.numel() == 2 * rows, \
+        "saved is what the forward pass returned"
+    result = {}
+    if want_dx:
+        result["dx"] = _dense_like(x, stream) if out is None else out
+    for name, t in (("dw", weight), ("db", bias)):
+        if t is not None and want_weight_grads:
+            result[name] = _dense_like(t, stream)
+    if "dw" in result or "db" in result:
+        need = int(lib().agent_layer_norm_bwd_workspace_bytes(ctypes.byref(desc)))
+        workspace = _ffn_workspace(need, workspace, stream, x.device)
+    st = lib().agent_layer_norm_bwd(ctypes.byref(desc), _norm_rows("x", x, x), _norm_rows("dy", dy, x), saved.data_ptr(), _ptr(weight),
+                                    _norm_rows("dsum", dsum, x), _ptr(workspace),
+                                    0 if workspace is None else workspace.numel() * workspace.element_size(),
+                                    _norm_rows("dx", result.get("dx"), x), _ptr(result.get("dw")), _ptr(result.get("db")),
+                                    _stream_on(stream, x.device))
+    _check(st, "agent_layer_norm_bwd")
+    return result
+
+
+@_on_its_device
+def prepare_layer_norm(x, weight=None, bias=None, *, residual=None, eps=1e-5, out, sum_out=None, stream=None) -> PreparedCall:
+    args = _layer_norm_args(x, weight, bias, residual, eps, None, out, sum_out, stream)
+    return PreparedCall(lib().agent_layer_norm_fwd, "agent_layer_norm_fwd", args, (x, weight, bias, residual, out, sum_out))

@@ -6,7 +6,9 @@
 
 #include "common.h"
 #include "ffn.h"
+#include "layer_norm.h"
 #include "rotary.h"
+#include "softmax.h"
 
 namespace aa {
 
@@ -133,6 +135,25 @@ hipError_t launch_rotary_bf16(const RotaryArgs& a, int ve, const RotaryPlan& p, 
 size_t rotary_partial_floats(const RotaryArgs& a);
 // dw_q, dw_k: gradients of the norm's weights, backward pass alone, null where they are not wanted
 hipError_t launch_rotary(int dtype, RotaryArgs& a, const RotaryShape& s, RotaryMode mode, float* dw_q, float* dw_k, hipStream_t st);
+
+// --- softmax attention: softmax.hip, and two units per element type ---
+hipError_t launch_softmax_f32(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st);
+hipError_t launch_softmax_f16(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st);
+hipError_t launch_softmax_bf16(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st);
+hipError_t launch_softmax_bwd_f32(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st);
+hipError_t launch_softmax_bwd_f16(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st);
+hipError_t launch_softmax_bwd_bf16(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st);
+// whether the blocks of these sizes can be numbered; workspaces (tensors without an address: of any alignment); launches
+bool softmax_fits(const SoftmaxArgs& a);
+size_t softmax_fwd_workspace(int dtype, const SoftmaxArgs& a);
+size_t softmax_bwd_workspace(int dtype, const SoftmaxArgs& a);
+hipError_t launch_softmax_fwd(int dtype, SoftmaxArgs a, void* workspace, hipStream_t st);
+hipError_t launch_softmax_bwd(int dtype, SoftmaxArgs a, void* workspace, hipStream_t st);
+
+// --- layer norm: one unit per element type; dw, db: the weights' gradients, in their type, null where they are not wanted ---
+hipError_t launch_layer_norm_f32(const NormArgs& a, const NormShape& s, bool back, void* dw, void* db, hipStream_t st);
+hipError_t launch_layer_norm_f16(const NormArgs& a, const NormShape& s, bool back, void* dw, void* db, hipStream_t st);
+hipError_t launch_layer_norm_bf16(const NormArgs& a, const NormShape& s, bool back, void* dw, void* db, hipStream_t st);
 
 // --- the gated feed-forward block: ffn.hip, and one unit per element type ---
 hipError_t launch_ffn_product_f32(const FfnGroup& g, FfnForm form, FfnEpilogue epi, int rows, int cols, hipStream_t st);

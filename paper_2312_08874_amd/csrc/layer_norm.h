@@ -1,0 +1,54 @@
+// Layer norm: what the C-ABI layer hands to the kernels, and the rule that shares a row out among lanes.  Plain C++ with no GPU
+// dependency, so that the rule can be tested without a GPU.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+namespace aa {
+
+constexpr int kNormWidth = 32768;      // most channels of a row
+
+struct NormRows {      // rows of a tensor: stride in elements
+  char* data;
+  long long stride;
+};
+
+struct NormArgs {
+  NormRows x, r, y, sum;              // forward; backward: x is the normed sum
+  NormRows dy, dsum, dx;              // backward
+  const void *w, *b;                  // in fp32 or the element type
+  int wide_weights;                   // 1: fp32
+  float2* stats;                      // [rows]: mean, 1 / deviation
+  int rows, width;
+  float eps, inv;                     // inv = 1 / width
+  float* partial;                     // backward: [block][2][width], sums of dy h and of dy
+  int blocks;
+};
+
+// A lane takes 16 bytes at a time, `pieces` times, `lanes` of them a row (a power of two up to a wave, or a whole block of 256 or 1024).
+struct NormShape {
+  int lanes, pieces, threads;
+  int rows_at_once() const { return lanes >= threads ? 1 : threads / lanes; }
+};
+// At most 32 channels a lane, whose sums of the weights' gradients stay in registers.
+inline NormShape norm_shape(int es, int width) {
+  const int per = 16 / es, most = 32 / per, count = (width + per - 1) / per;
+  NormShape s{64, 1, 256};
+  if (count > 256 * most) s.lanes = s.threads = 1024;
+  else if (count > 64 * most) s.lanes = 256;
+  else
+    while (s.lanes > 1 && s.lanes / 2 * 2 >= count) s.lanes /= 2;      // two pieces a lane where rows are short
+  while (s.lanes * s.pieces < count) s.pieces *= 2;
+  return s;
+}
+
+// Blocks of the backward pass, each of which leaves a part of the weights' gradients.
+constexpr int kNormBlocks = 512;
+inline int norm_blocks(const NormShape& s, int rows, bool backward) {
+  const long long needed = ((long long)rows + s.rows_at_once() - 1) / s.rows_at_once();
+  return (int)std::min<long long>(needed, backward ? kNormBlocks : 2048);
+}
+
+}  // namespace aa

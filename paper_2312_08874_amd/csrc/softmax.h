@@ -1,0 +1,101 @@
+// Softmax attention: what the C-ABI layer hands to the kernels, and the rules that choose among them.  Plain C++ with no GPU
+// dependency, so that the rules can be tested without a GPU.
+#pragma once
+#include <stddef.h>
+#include <stdint.h>
+
+#include <algorithm>
+
+#include "rotary.h"      // TokenView
+
+namespace aa {
+
+constexpr int kSoftmaxWidth = 256;      // most channels of a head
+
+struct SoftmaxArgs {
+  TokenView q, k, v, out, dout, dq, dk, dv;
+  float* lse;           // [batch][heads_q][tokens_q], natural logarithm; null: not wanted
+  const int *starts_q, *starts_k;        // packed: [sequences + 1], batch 1
+  const int *lengths_q, *lengths_k;      // padded: [batch], or null: every row
+  int batch, heads_q, heads_k, tokens_q, tokens_k, d, sequences;      // sequences 0: not packed
+  int causal;
+  int wide;             // whole 16-byte pieces wherever a result is stored
+  float scale, c;       // c = scale log2 e
+  // columns kernel: query heads side by side in a tile, tokens of a tile, ranges of keys and where each leaves its part
+  int pack, tile_tokens, splits;
+  float *part, *part_ml;      // [split][batch, head, token][d], [..][2]
+  // backward pass: what the queries' kernel leaves for the keys' of every query, [2][batch][heads_q][tokens_q], and fp16's peaks
+  float* stats;
+  unsigned* peaks;      // bits of the largest squared length of a row of dout, and of v
+  // parts of dq, or of dk and dv: [split][batch, head, token][d]
+  float *part_a, *part_b;
+};
+
+// Width that the kernels are compiled for: a multiple of the matrix instruction's 32 rows.
+inline int softmax_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
+
+// Tiles of `rows` tokens along the queries (or keys) of all sequences together; sequence s of a packed run has the tiles from
+// starts[s] / rows + s on, which leaves each at least the tiles it needs, whatever the lengths on the device are.
+inline long long softmax_tiles(int tokens, int batch, int sequences, int rows) {
+  return sequences > 0 ? (long long)tokens / rows + sequences : (long long)batch * (((long long)tokens + rows - 1) / rows);
+}
+
+// A tile of keys (or of queries, for the keys' kernel) on its way through LDS, and the tokens that a block's waves take side by side.
+constexpr int softmax_step(int es) { return es == 4 ? 32 : 64; }
+constexpr int kSoftmaxRowWaves = 4;
+inline int softmax_row_block() { return 32 * kSoftmaxRowWaves; }
+// Waves of a columns block: as many as 160 KB of LDS hold two tiles of 32 keys of.
+constexpr int softmax_column_waves(int es, int dp) { return es * dp <= 256 ? 4 : es * dp <= 512 ? 2 : 1; }
+
+constexpr int kSoftmaxUnits = 256;      // compute units
+
+struct SoftmaxPlan {
+  bool columns;
+  int pack, tile_tokens, splits;
+  long long tiles;      // of queries
+};
+// Ranges that make up for blocks that are too few, each of `least` keys at the least.
+inline int softmax_splits(long long blocks, long long wanted, long long keys, int least) {
+  const long long most = std::max(1ll, keys / least);
+  return (int)std::min(std::min(most, 128ll), std::max(1ll, (wanted + blocks - 1) / std::max(1ll, blocks)));
+}
+// keys (or queries) of a sequence, as far as the host knows
+inline long long softmax_typical(int tokens, int sequences) {
+  return sequences > 1 ? std::min<long long>(tokens, 2ll * tokens / sequences + 1) : tokens;
+}
+inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a) {
+  SoftmaxPlan p{};
+  const int group = a.heads_q / a.heads_k, outer = a.sequences > 0 ? 1 : a.batch;
+  const long long queries = softmax_typical(a.tokens_q, a.sequences), keys = softmax_typical(a.tokens_k, a.sequences);
+  const long long row_blocks = softmax_tiles(a.tokens_q, a.batch, a.sequences, softmax_row_block()) * a.heads_q;
+  p.columns = queries <= 32 || row_blocks < kSoftmaxUnits;
+  p.pack = 1, p.tile_tokens = softmax_row_block(), p.splits = 1;
+  if (p.columns) {
+    // heads that share keys side by side, where the tokens leave room
+    if (queries * 2 <= 32)
+      for (int n = 2; n <= group && n <= 32; ++n)
+        if (group % n == 0 && (queries * n <= 32 || n <= 4)) p.pack = n;
+    p.tile_tokens = 32 / p.pack;
+  }
+  p.tiles = softmax_tiles(a.tokens_q, outer, a.sequences, p.tile_tokens);
+  if (a.sequences == 0) p.tiles /= outer;
+  if (p.columns) {
+    const long long blocks = p.tiles * outer * a.heads_q / p.pack;
+    p.splits = softmax_splits(blocks, 4 * kSoftmaxUnits, keys, 512);
+  }
+  return p;
+}
+// Ranges of the backward pass: of keys for the queries' kernel, of queries (all heads that share the keys) for the keys'.
+inline int softmax_dq_splits(const SoftmaxArgs& a) {
+  return softmax_splits(softmax_tiles(a.tokens_q, a.batch, a.sequences, softmax_row_block()) * a.heads_q, 2 * kSoftmaxUnits,
+                        softmax_typical(a.tokens_k, a.sequences), 512);
+}
+inline int softmax_dkv_splits(const SoftmaxArgs& a) {
+  return softmax_splits(softmax_tiles(a.tokens_k, a.batch, a.sequences, softmax_row_block()) * a.heads_k, 2 * kSoftmaxUnits,
+                        softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k), 512);
+}
+
+// Launches of one element type (softmax_{bf16,f16,f32}.hip, and softmax_bwd_*).
+enum class SoftmaxPass { kRows, kColumns, kJoin, kPeaks, kQueries, kKeys, kSumQueries, kSumKeys };
+
+}  // namespace aa

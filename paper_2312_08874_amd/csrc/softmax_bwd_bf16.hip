@@ -1,0 +1,7 @@
+#include "softmax_bwd_kernels.inc"
+
+namespace aa {
+hipError_t launch_softmax_bwd_bf16(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st) {
+  return dispatch_backward<ElemBF16>(a, pass, tiles, st);
+}
+}  // namespace aa

@@ -1,0 +1,95 @@
+"""Layer norm with the residual sum on the GPU, forward and backward, against its definition in 64 bits; bounds:
+layer_norm_reference."""
+import pytest
+import torch
+
+from tests import layer_norm_reference as ref
+
+pytestmark = pytest.mark.gpu
+DT = {"f32": torch.float32, "f16": torch.float16, "bf16": torch.bfloat16}
+
+
+def close(got, want, what):
+    value, bound = want
+    got = got.double().cpu()
+    assert got.shape == value.shape, what
+    assert bool(torch.isfinite(got).all()), what + ": not finite"
+    off = (got - value).abs() - bound
+    assert bool((off <= 0).all()), "%s: off by %.3g more than allowed, at %d of %d" % (what, off.max(), int((off > 0).sum()), off.numel())
+
+
+# dtype, rows, width, residual, weights ("", "w", "wb"), their type, layout
+CASES = [
+    ("bf16", 5, 192, True, "wb", "x", "dense"),
+    ("f16", 300, 512, False, "wb", "f32", "dense"),
+    ("f32", 77, 288, True, "wb", "f32", "dense"),
+    ("bf16", 1, 1, True, "wb", "x", "dense"),
+    ("f16", 3, 2, False, "w", "x", "dense"),
+    ("f32", 1030, 5, False, "wb", "f32", "dense"),
+    ("bf16", 2100, 16, True, "", "x", "dense"),
+    ("bf16", 33, 1365, True, "wb", "f32", "dense"),
+    ("f16", 9, 2049, False, "wb", "x", "dense"),
+    ("f32", 9, 1031, True, "w", "f32", "dense"),
+    ("bf16", 4, 4096, True, "wb", "x", "dense"),
+    ("f16", 3, 8192, True, "wb", "f32", "dense"),
+    ("f32", 3, 8192, False, "wb", "f32", "dense"),
+    ("bf16", 3, 16384, True, "wb", "x", "dense"),
+    ("f16", 2, 32768, False, "wb", "x", "dense"),
+    ("f32", 2, 32768, True, "wb", "f32", "dense"),
+    ("bf16", 2, 20001, False, "wb", "f32", "dense"),
+    ("f32", 2, 9001, False, "", "f32", "dense"),
+    ("f16", 40, 96, True, "wb", "x", "columns"),
+    ("bf16", 40, 101, True, "wb", "f32", "odd"),
+    ("f32", 40, 130, False, "w", "f32", "odd"),
+    ("bf16", 5000, 64, True, "wb", "f32", "dense"),
+    ("f16", 4100, 640, False, "wb", "x", "dense"),
+    ("f32", 2500, 1024, False, "wb", "f32", "dense"),
+]
+
+
+def rows_of(gen, dtype, T, C, layout, std=1.0, mean=0.0):
+    def rnd(*shape):
+        return (mean + std * torch.randn(*shape, generator=gen)).to(dtype).cuda()
+    if layout == "dense":
+        return rnd(T, C)
+    if layout == "columns":
+        return rnd(T, 3 * C)[:, C:2 * C]
+    return rnd(T, C + 3)[:, 1:C + 1]
+
+
+def _inputs(case, std=1.0, mean=0.5, seed=4):
+    dtype, T, C, residual, weights, wtype, layout = case
+    gen = torch.Generator().manual_seed(seed)
+    wt = torch.float32 if wtype == "f32" else DT[dtype]
+    x = rows_of(gen, DT[dtype], T, C, layout, std, mean)
+    r = rows_of(gen, DT[dtype], T, C, layout, std) if residual else None
+    w = (1 + 0.3 * torch.randn(C, generator=gen)).to(wt).cuda() if "w" in weights else None
+    b = (0.3 * torch.randn(C, generator=gen)).to(wt).cuda() if "b" in weights else None
+    dy = rows_of(gen, DT[dtype], T, C, layout)
+    ds = rows_of(gen, DT[dtype], T, C, layout) if residual else None
+    return x, r, w, b, dy, ds
+
+
+@pytest.mark.parametrize("case", CASES, ids=[str(i) for i in range(len(CASES))])
+def test_norm_and_its_gradients(case):
+    from paper_2312_08874_amd import binding
+    x, r, w, b, dy, ds = _inputs(case)
+    eps = 1e-5
+    y, *rest = binding.agent_layer_norm_fwd(x, w, b, residual=r, eps=eps, save=True)
+    want = ref.forward(x, w, b, eps, r)
+    close(y, want["y"], "y")
+    s = x
+    if r is not None:
+        s = rest[0]
+        close(s, want["sum"], "sum")
+    # the backward pass norms the rounded sum; its statistics are those of what was normed
+    _, stats = binding.agent_layer_norm_fwd(s, w, b, eps=eps, save=True)
+    grads = binding.agent_layer_norm_bwd(s, dy, stats, w, b, dsum=ds)
+    expected = ref.backward(s, dy, w, b, eps, ds)
+    assert set(grads) == set(expected)
+    for name in grads:
+        close(grads[name], expected[name], name)
+    more = binding.agent_layer_norm_bwd(s, dy, stats, w, b, dsum=ds)
+    assert all(torch.equal(grads[n], more[n]) for n in grads)
+    alone = binding.agent_layer_norm_fwd(x, w, b, residual=r, eps=eps)
+    assert torch.equal(alone if r is None else alone[0], y)
