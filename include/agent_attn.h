@@ -437,22 +437,25 @@ typedef struct {
   float scale;                     /* 0: d^-1/2 */
 } aa_softmax_attn;
 
-/* Bytes of device workspace of either pass, which may be 0 for the forward pass.  Tensors whose rows are no whole, aligned 16-byte
+/* Bytes of what the forward pass keeps, and of device workspace of either pass, which may be 0 for the forward pass.  Tensors whose rows are no whole, aligned 16-byte
  * pieces are copied there first; a view that is NULL counts as one of them.  0 for an invalid descriptor. */
+size_t agent_softmax_attn_saved_bytes(const aa_softmax_attn *desc);
 size_t agent_softmax_attn_workspace_bytes(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v);
 size_t agent_softmax_attn_bwd_workspace_bytes(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
                                               const aa_view *dout);
-/* lse: NULL, or [batch][heads_q][tokens_q] for the backward pass.  Results overlap nothing (slices of one buffer as above).
+/* saved: NULL, or agent_softmax_attn_saved_bytes() of device memory, 256-byte aligned, for the backward pass: lse, fp32,
+ * [batch][heads_q][tokens_q], from the start on, and for 16-bit types what rounding took from out, which D below is off without where
+ * rows see few keys (its gradients by twice their rounding).  Results overlap nothing (slices of one buffer as above).
  * Errors: AA_ERR_NULL, AA_ERR_SHAPE, AA_ERR_DTYPE, AA_ERR_UNSUPPORTED (d > 256, more blocks or elements than can be numbered),
  * AA_ERR_WORKSPACE (256-byte aligned), AA_ERR_ALIAS. */
 aa_status agent_softmax_attn_fwd(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
-                                 void *workspace, size_t workspace_bytes, const aa_view *out, float *lse, void *hip_stream);
-/* Gradients for the gradient dout of out, from what the forward pass read and left:
+                                 void *workspace, size_t workspace_bytes, const aa_view *out, void *saved, void *hip_stream);
+/* Gradients for the gradient dout of out, from what the forward pass read, wrote and kept:
  *   D_i = dout_i . out_i,  ds_ij = p_ij (dout_i . v_j - D_i),
  *   dq_i = scale sum over j of ds_ij k_j,  dk_j = scale sum over i of ds_ij q_i,  dv_j = sum over i of p_ij dout_i,
  * the last two over all query heads that share the keys.  The same inputs give the same bits. */
 aa_status agent_softmax_attn_bwd(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
-                                 const aa_view *out, const float *lse, const aa_view *dout, void *workspace,
+                                 const aa_view *out, const void *saved, const aa_view *dout, void *workspace,
                                  size_t workspace_bytes, const aa_view *dq, const aa_view *dk, const aa_view *dv,
                                  void *hip_stream);
 

@@ -111,7 +111,7 @@ EXPORTS = ("agent_attn_workspace_bytes", "agent_attn_fwd", "agent_pool_fwd", "ag
            "agent_attn_module_fwd", "agent_rope_fwd", "agent_rope_bwd", "agent_qk_norm_fwd", "agent_qk_norm_bwd",
            "agent_qk_norm_bwd_workspace_bytes", "agent_gated_ffn_workspace_bytes", "agent_gated_ffn_saved_bytes",
            "agent_gated_ffn_bwd_workspace_bytes", "agent_gated_ffn_fwd", "agent_gated_ffn_bwd",
-           "agent_softmax_attn_workspace_bytes", "agent_softmax_attn_bwd_workspace_bytes", "agent_softmax_attn_fwd",
+           "agent_softmax_attn_saved_bytes", "agent_softmax_attn_workspace_bytes", "agent_softmax_attn_bwd_workspace_bytes", "agent_softmax_attn_fwd",
            "agent_softmax_attn_bwd", "agent_layer_norm_fwd", "agent_layer_norm_bwd_workspace_bytes", "agent_layer_norm_bwd")
 
 _lib = None
@@ -191,6 +191,8 @@ def lib():
         L.agent_gated_ffn_bwd.restype = ctypes.c_int
         L.agent_gated_ffn_bwd.argtypes = [fp, vp, wp, vp, vp, vp, ctypes.c_size_t, vp, gp, vp]
         sp = ctypes.POINTER(aa_softmax_attn)
+        L.agent_softmax_attn_saved_bytes.restype = ctypes.c_size_t
+        L.agent_softmax_attn_saved_bytes.argtypes = [sp]
         L.agent_softmax_attn_workspace_bytes.restype = ctypes.c_size_t
         L.agent_softmax_attn_workspace_bytes.argtypes = [sp, tv, tv, tv]
         L.agent_softmax_attn_bwd_workspace_bytes.restype = ctypes.c_size_t
@@ -1022,14 +1024,15 @@ def _softmax_workspace(need, workspace, stream, device):
     return workspace
 
 
-def _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, lse, out, workspace, stream):
+def _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, save, out, workspace, stream):
     desc, (q, k, v) = _softmax_call(Q, K, V, causal, starts, lengths, scale)
     o = _checked_view("out", out, Q, Q.shape)
+    saved = _alloc_bytes(int(lib().agent_softmax_attn_saved_bytes(ctypes.byref(desc))), stream, Q.device) if save else None
     need = int(lib().agent_softmax_attn_workspace_bytes(ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v)))
     workspace = _softmax_workspace(need, workspace, stream, Q.device)
     return (ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v), _ptr(workspace),
-            0 if workspace is None else workspace.numel() * workspace.element_size(), ctypes.byref(o), _ptr(lse),
-            _stream_on(stream, Q.device)), (desc, q, k, v, o, workspace)
+            0 if workspace is None else workspace.numel() * workspace.element_size(), ctypes.byref(o), _ptr(saved),
+            _stream_on(stream, Q.device)), saved, (desc, q, k, v, o, workspace)
 
 
 @_on_its_device
@@ -1039,27 +1042,23 @@ def agent_softmax_attn_fwd(Q, K, V, *, causal=False, starts=None, lengths=None, 
     channels side by side.  causal: a query sees the keys up to its place from the end.  lengths: (of the queries, of the
     keys), int32 [B] on the device, either None: rows in use of every sequence.  starts: (of the queries, of the keys), int32
     [S+1] on the device: S sequences packed into one batch element's rows.  scale 0: d^-1/2.  save: also returns what
-    agent_softmax_attn_bwd needs, (out, lse).  Rows of no sequence: zeros, or what `out` held."""
-    import torch
+    agent_softmax_attn_bwd needs, (out, saved).  Rows of no sequence: zeros, or what `out` held."""
     if out is None:
         out = _fresh_tokens(Q, starts is not None or lengths is not None, stream)
-    lse = None
-    if save:
-        lse = _alloc_bytes(4 * Q.shape[0] * Q.shape[1] * Q.shape[2], stream, Q.device).view(torch.float32).view(Q.shape[:3])
-    args, keep = _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, lse, out, workspace, stream)
+    args, saved, keep = _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, save, out, workspace, stream)
     _check(lib().agent_softmax_attn_fwd(*args), "agent_softmax_attn_fwd")
-    return (out, lse) if save else out
+    return (out, saved) if save else out
 
 
 @_on_its_device
-def agent_softmax_attn_bwd(Q, K, V, out, lse, dO, *, causal=False, starts=None, lengths=None, scale=0.0, grads=None, workspace=None,
+def agent_softmax_attn_bwd(Q, K, V, out, saved, dO, *, causal=False, starts=None, lengths=None, scale=0.0, grads=None, workspace=None,
                            stream=None):
-    """Gradients of agent_softmax_attn_fwd for the gradient dO of its result `out`; lse: what it returned.  A dict of dQ, dK, dV.
+    """Gradients of agent_softmax_attn_fwd for the gradient dO of its result `out`; saved: what it returned.  A dict of dQ, dK, dV.
     grads: (dQ, dK, dV) to write to, whose rows of no sequence stay as they are (fresh ones: zeros)."""
     import torch
     desc, (q, k, v) = _softmax_call(Q, K, V, causal, starts, lengths, scale)
-    assert lse.get_device() == Q.get_device() and lse.dtype == torch.float32 and lse.is_contiguous() and lse.shape == Q.shape[:3], \
-        "lse is what the forward pass returned"
+    assert saved.get_device() == Q.get_device() and saved.dtype == torch.uint8 and saved.is_contiguous() and \
+        saved.numel() >= int(lib().agent_softmax_attn_saved_bytes(ctypes.byref(desc))), "saved is what the forward pass returned"
     o, g = _checked_view("out", out, Q, Q.shape), _checked_view("dO", dO, Q, Q.shape)
     if grads is None:
         grads = tuple(_fresh_tokens(t, starts is not None or lengths is not None, stream) for t in (Q, K, V))
@@ -1068,7 +1067,7 @@ def agent_softmax_attn_bwd(Q, K, V, out, lse, dO, *, causal=False, starts=None, 
                                                             ctypes.byref(g)))
     workspace = _softmax_workspace(need, workspace, stream, Q.device)
     st = lib().agent_softmax_attn_bwd(ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v), ctypes.byref(o),
-                                      lse.data_ptr(), ctypes.byref(g), _ptr(workspace),
+                                      saved.data_ptr(), ctypes.byref(g), _ptr(workspace),
                                       0 if workspace is None else workspace.numel() * workspace.element_size(), ctypes.byref(dq),
                                       ctypes.byref(dk), ctypes.byref(dv), _stream_on(stream, Q.device))
     _check(st, "agent_softmax_attn_bwd")
@@ -1078,7 +1077,7 @@ def agent_softmax_attn_bwd(Q, K, V, out, lse, dO, *, causal=False, starts=None, 
 @_on_its_device
 def prepare_softmax_attn(Q, K, V, *, causal=False, starts=None, lengths=None, scale=0.0, out, workspace=None, stream=None) -> PreparedCall:
     """The lengths or starts may change on the device between the calls."""
-    args, keep = _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, None, out, workspace, stream)
+    args, _, keep = _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, False, out, workspace, stream)
     return PreparedCall(lib().agent_softmax_attn_fwd, "agent_softmax_attn_fwd", args, (keep, Q, K, V, starts, lengths, out))
 
 

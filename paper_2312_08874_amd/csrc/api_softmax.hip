@@ -80,11 +80,19 @@ bool any_meet(const TokenSpan (&results)[R], const TokenSpan (&inputs)[I], const
   return false;
 }
 
-size_t lse_bytes(const aa_softmax_attn* d) { return (size_t)4 * d->batch * d->heads_q * d->tokens_q; }
+// what the forward pass keeps: its place
+void keep(const aa_softmax_attn* d, const void* saved, SoftmaxArgs* a) {
+  a->lse = (float*)const_cast<void*>(saved);
+  a->low = saved && d->dtype != AA_F32 ? (char*)const_cast<void*>(saved) + aa::softmax_saved_lse(*a) : nullptr;
+}
 
 }  // namespace
 
 extern "C" {
+
+size_t agent_softmax_attn_saved_bytes(const aa_softmax_attn* desc) {
+  return check_desc(desc) == AA_OK ? aa::softmax_saved_bytes(desc->dtype, args_of(desc)) : 0;
+}
 
 size_t agent_softmax_attn_workspace_bytes(const aa_softmax_attn* desc, const aa_view* q, const aa_view* k, const aa_view* v) {
   if (check_desc(desc) != AA_OK) return 0;
@@ -109,7 +117,7 @@ size_t agent_softmax_attn_bwd_workspace_bytes(const aa_softmax_attn* desc, const
 }
 
 aa_status agent_softmax_attn_fwd(const aa_softmax_attn* desc, const aa_view* q, const aa_view* k, const aa_view* v, void* workspace,
-                                 size_t workspace_bytes, const aa_view* out, float* lse, void* hip_stream) {
+                                 size_t workspace_bytes, const aa_view* out, void* saved, void* hip_stream) {
   aa_status st = check_desc(desc);
   if (st != AA_OK) return st;
   SoftmaxArgs a = args_of(desc);
@@ -118,25 +126,25 @@ aa_status agent_softmax_attn_fwd(const aa_softmax_attn* desc, const aa_view* q, 
   if ((st = take(desc, k, true, false, &in[1], &a.k)) != AA_OK) return st;
   if ((st = take(desc, v, true, false, &in[2], &a.v)) != AA_OK) return st;
   if ((st = take(desc, out, false, true, &res[0], &a.out)) != AA_OK) return st;
-  if ((uintptr_t)lse & 3) return AA_ERR_SHAPE;
-  if (!aa::softmax_fits(a)) return AA_ERR_UNSUPPORTED;
+  if (!aa::softmax_fits(desc->dtype, a)) return AA_ERR_UNSUPPORTED;
+  if ((uintptr_t)saved % kAlign) return AA_ERR_WORKSPACE;
   const size_t need = aa::softmax_fwd_workspace(desc->dtype, a);
   if (need > 0 && (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < need)) return AA_ERR_WORKSPACE;
   const size_t ns = desc->sequences > 0 ? (size_t)4 * (desc->sequences + 1) : 0, nl = (size_t)4 * desc->batch;
-  const Bytes written[] = {{workspace, need}, {lse, lse_bytes(desc)}};
+  const Bytes written[] = {{workspace, need}, {saved, aa::softmax_saved_bytes(desc->dtype, a)}};
   const Bytes read[] = {{desc->starts_q, ns}, {desc->starts_k, ns}, {desc->lengths_q, nl}, {desc->lengths_k, nl}};
   if (any_meet(res, in, written, read)) return AA_ERR_ALIAS;
-  a.lse = lse;
+  keep(desc, saved, &a);
   return aa::launch_softmax_fwd(desc->dtype, a, workspace, (hipStream_t)hip_stream) == hipSuccess ? AA_OK : AA_ERR_HIP;
 }
 
 aa_status agent_softmax_attn_bwd(const aa_softmax_attn* desc, const aa_view* q, const aa_view* k, const aa_view* v, const aa_view* out,
-                                 const float* lse, const aa_view* dout, void* workspace, size_t workspace_bytes, const aa_view* dq,
+                                 const void* saved, const aa_view* dout, void* workspace, size_t workspace_bytes, const aa_view* dq,
                                  const aa_view* dk, const aa_view* dv, void* hip_stream) {
   aa_status st = check_desc(desc);
   if (st != AA_OK) return st;
-  if (!lse) return AA_ERR_NULL;
-  if ((uintptr_t)lse & 3) return AA_ERR_SHAPE;
+  if (!saved) return AA_ERR_NULL;
+  if ((uintptr_t)saved % kAlign) return AA_ERR_WORKSPACE;
   SoftmaxArgs a = args_of(desc);
   TokenSpan in[5], res[3];
   if ((st = take(desc, q, false, false, &in[0], &a.q)) != AA_OK) return st;
@@ -147,14 +155,14 @@ aa_status agent_softmax_attn_bwd(const aa_softmax_attn* desc, const aa_view* q, 
   if ((st = take(desc, dq, false, true, &res[0], &a.dq)) != AA_OK) return st;
   if ((st = take(desc, dk, true, true, &res[1], &a.dk)) != AA_OK) return st;
   if ((st = take(desc, dv, true, true, &res[2], &a.dv)) != AA_OK) return st;
-  if (!aa::softmax_fits(a)) return AA_ERR_UNSUPPORTED;
+  if (!aa::softmax_fits(desc->dtype, a)) return AA_ERR_UNSUPPORTED;
   const size_t need = aa::softmax_bwd_workspace(desc->dtype, a);
   if (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < need) return AA_ERR_WORKSPACE;
   const size_t ns = desc->sequences > 0 ? (size_t)4 * (desc->sequences + 1) : 0, nl = (size_t)4 * desc->batch;
   const Bytes written[] = {{workspace, need}};
-  const Bytes read[] = {{lse, lse_bytes(desc)}, {desc->starts_q, ns}, {desc->starts_k, ns}, {desc->lengths_q, nl}, {desc->lengths_k, nl}};
+  const Bytes read[] = {{saved, aa::softmax_saved_bytes(desc->dtype, a)}, {desc->starts_q, ns}, {desc->starts_k, ns}, {desc->lengths_q, nl}, {desc->lengths_k, nl}};
   if (any_meet(res, in, written, read)) return AA_ERR_ALIAS;
-  a.lse = const_cast<float*>(lse);
+  keep(desc, saved, &a);
   return aa::launch_softmax_bwd(desc->dtype, a, workspace, (hipStream_t)hip_stream) == hipSuccess ? AA_OK : AA_ERR_HIP;
 }
 

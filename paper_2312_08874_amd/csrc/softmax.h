@@ -14,11 +14,15 @@ constexpr int kSoftmaxWidth = 256;      // most channels of a head
 
 struct SoftmaxArgs {
   TokenView q, k, v, out, dout, dq, dk, dv;
-  float* lse;           // [batch][heads_q][tokens_q], natural logarithm; null: not wanted
+  // what the forward pass keeps, null: nothing: lse (natural logarithm) [batch][heads_q][tokens_q] and, of 16-bit types, what
+  // rounding took from out, [..][d], itself in the type
+  float* lse;
+  char* low;
   const int *starts_q, *starts_k;        // packed: [sequences + 1], batch 1
   const int *lengths_q, *lengths_k;      // padded: [batch], or null: every row
   int batch, heads_q, heads_k, tokens_q, tokens_k, d, sequences;      // sequences 0: not packed
   int causal;
+  int waves;            // of a block: 2, 4 or 8, each of which has 32 rows
   int wide;             // whole 16-byte pieces wherever a result is stored
   float scale, c;       // c = scale log2 e
   // columns kernel: query heads side by side in a tile, tokens of a tile, ranges of keys and where each leaves its part
@@ -29,6 +33,7 @@ struct SoftmaxArgs {
   unsigned* peaks;      // bits of the largest squared length of a row of dout, and of v
   // parts of dq, or of dk and dv: [split][batch, head, token][d]
   float *part_a, *part_b;
+  int first_batch;      // of a launch that sums them
 };
 
 // Width that the kernels are compiled for: a multiple of the matrix instruction's 32 rows.
@@ -42,14 +47,24 @@ inline long long softmax_tiles(int tokens, int batch, int sequences, int rows) {
 
 // A tile of keys (or of queries, for the keys' kernel) on its way through LDS, and the tokens that a block's waves take side by side.
 constexpr int softmax_step(int es) { return es == 4 ? 32 : 64; }
-constexpr int kSoftmaxRowWaves = 4;
-inline int softmax_row_block() { return 32 * kSoftmaxRowWaves; }
 // Waves of a columns block: as many as 160 KB of LDS hold two tiles of 32 keys of.
 constexpr int softmax_column_waves(int es, int dp) { return es * dp <= 256 ? 4 : es * dp <= 512 ? 2 : 1; }
 
 constexpr int kSoftmaxUnits = 256;      // compute units
 
+// Waves of a block of rows, 32 rows each: MEASURED
+constexpr int softmax_most_waves(int es, int d) { return es == 2 && d > 32 && d <= 128 ? 8 : 4; }
+inline int softmax_waves(int tokens, int batch, int sequences, int heads, int most) {
+  auto rounds = [&](int waves) {
+    const long long blocks = softmax_tiles(tokens, batch, sequences, 32 * waves) * heads;
+    return (blocks + kSoftmaxUnits - 1) / kSoftmaxUnits * waves;
+  };
+  const int waves = rounds(2) < rounds(4) ? 2 : 4;
+  return most >= 8 && rounds(8) <= rounds(waves) ? 8 : waves;
+}
+
 struct SoftmaxPlan {
+  int waves;
   bool columns;
   int pack, tile_tokens, splits;
   long long tiles;      // of queries
@@ -63,13 +78,14 @@ inline int softmax_splits(long long blocks, long long wanted, long long keys, in
 inline long long softmax_typical(int tokens, int sequences) {
   return sequences > 1 ? std::min<long long>(tokens, 2ll * tokens / sequences + 1) : tokens;
 }
-inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a) {
+inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a, int es) {
   SoftmaxPlan p{};
   const int group = a.heads_q / a.heads_k, outer = a.sequences > 0 ? 1 : a.batch;
   const long long queries = softmax_typical(a.tokens_q, a.sequences), keys = softmax_typical(a.tokens_k, a.sequences);
-  const long long row_blocks = softmax_tiles(a.tokens_q, a.batch, a.sequences, softmax_row_block()) * a.heads_q;
+  p.waves = softmax_waves(a.tokens_q, a.batch, a.sequences, a.heads_q, softmax_most_waves(es, a.d));
+  const long long row_blocks = softmax_tiles(a.tokens_q, a.batch, a.sequences, 128) * a.heads_q;
   p.columns = queries <= 32 || row_blocks < kSoftmaxUnits;
-  p.pack = 1, p.tile_tokens = softmax_row_block(), p.splits = 1;
+  p.pack = 1, p.tile_tokens = 32 * p.waves, p.splits = 1;
   if (p.columns) {
     // heads that share keys side by side, where the tokens leave room
     if (queries * 2 <= 32)
@@ -85,14 +101,19 @@ inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a) {
   }
   return p;
 }
-// Ranges of the backward pass: of keys for the queries' kernel, of queries (all heads that share the keys) for the keys'.
-inline int softmax_dq_splits(const SoftmaxArgs& a) {
-  return softmax_splits(softmax_tiles(a.tokens_q, a.batch, a.sequences, softmax_row_block()) * a.heads_q, 2 * kSoftmaxUnits,
-                        softmax_typical(a.tokens_k, a.sequences), 512);
-}
-inline int softmax_dkv_splits(const SoftmaxArgs& a) {
-  return softmax_splits(softmax_tiles(a.tokens_k, a.batch, a.sequences, softmax_row_block()) * a.heads_k, 2 * kSoftmaxUnits,
-                        softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k), 512);
+// The backward pass: ranges of keys for the queries' kernel, of queries (all heads that share the keys) for the keys'.
+struct SoftmaxBackPlan {
+  int waves, splits;
+  long long tiles;      // of one sequence, or of the packed run
+};
+inline SoftmaxBackPlan softmax_back_plan(const SoftmaxArgs& a, int es, bool keys) {
+  const int tokens = keys ? a.tokens_k : a.tokens_q, heads = keys ? a.heads_k : a.heads_q;
+  SoftmaxBackPlan p;
+  p.waves = softmax_waves(tokens, a.batch, a.sequences, heads, keys ? 4 : softmax_most_waves(es, a.d));
+  p.tiles = softmax_tiles(tokens, 1, a.sequences, 32 * p.waves);
+  p.splits = softmax_splits(p.tiles * (a.sequences > 0 ? 1 : a.batch) * heads, 2 * kSoftmaxUnits,
+                            keys ? softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k) : softmax_typical(a.tokens_k, a.sequences), 512);
+  return p;
 }
 
 // Launches of one element type (softmax_{bf16,f16,f32}.hip, and softmax_bwd_*).

@@ -59,9 +59,6 @@ hipError_t launch(int dtype, const SoftmaxArgs& a, SoftmaxPass pass, long long t
 
 long long query_rows(const SoftmaxArgs& a) { return (long long)a.batch * a.heads_q * a.tokens_q; }
 long long key_rows(const SoftmaxArgs& a) { return (long long)a.batch * a.heads_k * a.tokens_k; }
-// tiles of one sequence, or of the packed run
-long long tiles_of(const SoftmaxArgs& a, int tokens) { return softmax_tiles(tokens, 1, a.sequences, softmax_row_block()); }
-
 bool wide_result(const TokenView& v, int batch, int heads, int tokens, int d, int es) {
   const unsigned long long strides = (batch > 1 ? v.sb : 0) | (heads > 1 ? v.sh : 0) | (tokens > 1 ? v.sn : 0);
   return d * es % 16 == 0 && (uintptr_t)v.data % 16 == 0 && strides * es % 16 == 0;
@@ -69,18 +66,25 @@ bool wide_result(const TokenView& v, int batch, int heads, int tokens, int d, in
 
 }  // namespace
 
-bool softmax_fits(const SoftmaxArgs& a) {      // blocks are numbered in 32 bits
-  const SoftmaxPlan p = softmax_plan(a);
+bool softmax_fits(int dtype, const SoftmaxArgs& a) {      // blocks are numbered in 32 bits
+  const int es = dtype == 0 ? 4 : 2;
+  const SoftmaxPlan p = softmax_plan(a, es);
+  const SoftmaxBackPlan q = softmax_back_plan(a, es, false), k = softmax_back_plan(a, es, true);
   const long long outer = a.sequences > 0 ? 1 : a.batch, lim = 1ll << 30;
-  return p.tiles * outer * a.heads_q / p.pack * p.splits < lim && tiles_of(a, a.tokens_q) * outer * a.heads_q * 128 < lim * 4 &&
-         tiles_of(a, a.tokens_k) * outer * a.heads_k * 128 < lim * 4;
+  return p.tiles * outer * a.heads_q / p.pack * p.splits < lim && q.tiles * outer * a.heads_q * q.splits < lim &&
+         k.tiles * outer * a.heads_k * k.splits < lim;
+}
+
+size_t softmax_saved_lse(const SoftmaxArgs& a) { return aligned((size_t)query_rows(a) * 4); }
+size_t softmax_saved_bytes(int dtype, const SoftmaxArgs& a) {
+  return softmax_saved_lse(a) + (dtype == 0 ? 0 : aligned((size_t)query_rows(a) * a.d * 2));
 }
 
 size_t softmax_fwd_workspace(int dtype, const SoftmaxArgs& a) {
   const int es = dtype == 0 ? 4 : 2;
   size_t bytes = copy_bytes(a.q, a.batch, a.heads_q, a.tokens_q, a.d, es) + copy_bytes(a.k, a.batch, a.heads_k, a.tokens_k, a.d, es) +
                  copy_bytes(a.v, a.batch, a.heads_k, a.tokens_k, a.d, es);
-  const SoftmaxPlan p = softmax_plan(a);
+  const SoftmaxPlan p = softmax_plan(a, es);
   if (p.splits > 1) bytes += aligned((size_t)p.splits * query_rows(a) * a.d * 4) + aligned((size_t)p.splits * query_rows(a) * 8);
   return bytes;
 }
@@ -93,8 +97,8 @@ hipError_t launch_softmax_fwd(int dtype, SoftmaxArgs a, void* workspace, hipStre
   if (err == hipSuccess) err = copy_to(a.k, ws, a.batch, a.heads_k, a.tokens_k, a.d, es, st);
   if (err == hipSuccess) err = copy_to(a.v, ws, a.batch, a.heads_k, a.tokens_k, a.d, es, st);
   if (err != hipSuccess) return err;
-  const SoftmaxPlan p = softmax_plan(a);
-  a.pack = p.pack, a.tile_tokens = p.tile_tokens, a.splits = p.splits;
+  const SoftmaxPlan p = softmax_plan(a, es);
+  a.waves = p.waves, a.pack = p.pack, a.tile_tokens = p.tile_tokens, a.splits = p.splits;
   if (p.splits > 1) {
     a.part = (float*)ws;
     a.part_ml = (float*)(ws + aligned((size_t)p.splits * query_rows(a) * a.d * 4));
@@ -107,7 +111,7 @@ size_t softmax_bwd_workspace(int dtype, const SoftmaxArgs& a) {
   const int es = dtype == 0 ? 4 : 2;
   const size_t q = copy_bytes(a.q, a.batch, a.heads_q, a.tokens_q, a.d, es), k = copy_bytes(a.k, a.batch, a.heads_k, a.tokens_k, a.d, es),
                v = copy_bytes(a.v, a.batch, a.heads_k, a.tokens_k, a.d, es), g = copy_bytes(a.dout, a.batch, a.heads_q, a.tokens_q, a.d, es);
-  const int sq = softmax_dq_splits(a), sk = softmax_dkv_splits(a);
+  const int sq = softmax_back_plan(a, es, false).splits, sk = softmax_back_plan(a, es, true).splits;
   // the queries' parts are added up before the keys' are written
   const size_t parts = std::max(sq > 1 ? aligned((size_t)sq * query_rows(a) * a.d * 4) : 0,
                                 sk > 1 ? 2 * aligned((size_t)sk * key_rows(a) * a.d * 4) : 0);
@@ -128,14 +132,15 @@ hipError_t launch_softmax_bwd(int dtype, SoftmaxArgs a, void* workspace, hipStre
   if (err == hipSuccess) err = copy_to(a.dout, ws, a.batch, a.heads_q, a.tokens_q, a.d, es, st);
   if (err == hipSuccess && dtype == 1) err = launch(dtype, a, SoftmaxPass::kPeaks, 0, st);
   if (err != hipSuccess) return err;
-  a.splits = softmax_dq_splits(a);
+  const SoftmaxBackPlan q = softmax_back_plan(a, es, false), k = softmax_back_plan(a, es, true);
+  a.waves = q.waves, a.splits = q.splits;
   a.part_a = (float*)ws;
-  err = launch(dtype, a, SoftmaxPass::kQueries, tiles_of(a, a.tokens_q), st);
+  err = launch(dtype, a, SoftmaxPass::kQueries, q.tiles, st);
   if (err == hipSuccess && a.splits > 1) err = launch(dtype, a, SoftmaxPass::kSumQueries, 0, st);
   if (err != hipSuccess) return err;
-  a.splits = softmax_dkv_splits(a);
+  a.waves = k.waves, a.splits = k.splits;
   a.part_b = (float*)(ws + aligned((size_t)a.splits * key_rows(a) * a.d * 4));
-  err = launch(dtype, a, SoftmaxPass::kKeys, tiles_of(a, a.tokens_k), st);
+  err = launch(dtype, a, SoftmaxPass::kKeys, k.tiles, st);
   return err != hipSuccess || a.splits == 1 ? err : launch(dtype, a, SoftmaxPass::kSumKeys, 0, st);
 }
 

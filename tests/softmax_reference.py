@@ -78,11 +78,13 @@ def attention(q, k, v, causal, where, scale=None, do=None):
             if G is None:
                 continue
             g = G[b, h, rows]
+            # D takes o with what rounding took from it, rounded in its turn
+            off_o = do_o + (round_out if dtype == torch.float32 else round_out ** 2) * (o.abs() + do_o) + smallest(dtype)
             rel = 2 * a + u + (n + 8) * E + 2 * E * level.abs() + fine * n
             D = (g * o).sum(-1, keepdim=True)
             t = g @ z.t() - D
             dt = (d + 2) * E * (g.abs() @ z.abs().t() + (g * o).abs().sum(-1, keepdim=True)) + \
-                (g.abs() * res["out"][1][b, h, rows]).sum(-1, keepdim=True)
+                (g.abs() * off_o).sum(-1, keepdim=True)
             ds = p * t
             off_p = p * (rel + u) + (fine * 2.0 ** -12 * seen)
             off_s = p * (rel * t.abs() + dt) * (1 + u) + u * ds.abs() + (fine * peak * 2.0 ** -12 * seen) + 4 * E * p * (t.abs() + D.abs())
