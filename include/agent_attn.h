@@ -478,14 +478,14 @@ typedef struct {
  * y and sum may be the rows of x or of residual (same pointer and stride) and otherwise overlap nothing (AA_ERR_ALIAS). */
 aa_status agent_layer_norm_fwd(const aa_layer_norm *desc, const aa_rows *x, const aa_rows *residual, const void *weight,
                                const void *bias, const aa_rows *y, const aa_rows *sum, float *saved, void *hip_stream);
-/* Gradients, from the normed rows x (the sum, where there was a residual) and the gradient dy of y; dsum: NULL, or a gradient of s from
- * elsewhere, which is added:
+/* Gradients, from x and residual as the forward pass had them (or x: its rounded sum, residual NULL, which leaves h and dweight with
+ * the error of that rounding) and the gradient dy of y; dsum: NULL, or a gradient of s from elsewhere, which is added:
  *   g = dy weight,  dx = r (g - mean g - h mean(g h)) + dsum,  dweight = sum over the rows of dy h,  dbias = sum of dy
- * dx is the gradient of x and of residual; it may be the rows of x, dy or dsum.  dweight, dbias: in the weight's type; NULL, as dx:
+ * dx is the gradient of x and of residual; it may be the rows of x, residual, dy or dsum.  dweight, dbias: in the weight's type; NULL, as dx:
  * not wanted; summed in a fixed order.  workspace: needed for dweight, dbias alone, 256-byte aligned. */
 size_t agent_layer_norm_bwd_workspace_bytes(const aa_layer_norm *desc);
-aa_status agent_layer_norm_bwd(const aa_layer_norm *desc, const aa_rows *x, const aa_rows *dy, const float *saved,
-                               const void *weight, const aa_rows *dsum, void *workspace, size_t workspace_bytes,
+aa_status agent_layer_norm_bwd(const aa_layer_norm *desc, const aa_rows *x, const aa_rows *residual, const aa_rows *dy,
+                               const float *saved, const void *weight, const aa_rows *dsum, void *workspace, size_t workspace_bytes,
                                const aa_rows *dx, void *dweight, void *dbias, void *hip_stream);
 
 /* Static string for a status code. */

@@ -207,7 +207,7 @@ def lib():
         L.agent_layer_norm_bwd_workspace_bytes.restype = ctypes.c_size_t
         L.agent_layer_norm_bwd_workspace_bytes.argtypes = [lp]
         L.agent_layer_norm_bwd.restype = ctypes.c_int
-        L.agent_layer_norm_bwd.argtypes = [lp, ro, ro, vp, vp, ro, vp, ctypes.c_size_t, ro, vp, vp, vp]
+        L.agent_layer_norm_bwd.argtypes = [lp, ro, ro, ro, vp, vp, ro, vp, ctypes.c_size_t, ro, vp, vp, vp]
         L.agent_attn_status_str.restype = ctypes.c_char_p
         L.agent_attn_status_str.argtypes = [ctypes.c_int]
         _lib = L
@@ -1129,11 +1129,11 @@ def agent_layer_norm_fwd(x, weight=None, bias=None, *, residual=None, eps=1e-5, 
 
 
 @_on_its_device
-def agent_layer_norm_bwd(x, dy, saved, weight=None, bias=None, *, dsum=None, want_dx=True, want_weight_grads=True, out=None,
-                         workspace=None, stream=None):
-    """Gradients of agent_layer_norm_fwd for the gradient dy of its y; x: what was normed (s, with a residual), saved: what the forward
-    pass returned, dsum: a gradient of s from elsewhere, which is added.  A dict of dx (the gradient of x and of residual) and, for
-    the weights present and want_weight_grads, dw and db in their type.  out: dx, which may be x, dy or dsum."""
+def agent_layer_norm_bwd(x, dy, saved, weight=None, bias=None, *, residual=None, dsum=None, want_dx=True, want_weight_grads=True,
+                         out=None, workspace=None, stream=None):
+    """Gradients of agent_layer_norm_fwd for the gradient dy of its y; x and residual: as in the forward pass, or x: its rounded
+    sum (which leaves dw with the error of that rounding), saved: what it returned, dsum: a gradient of s from elsewhere, which is added.  A dict of dx (the gradient of x and of residual) and, for
+    the weights present and want_weight_grads, dw and db in their type.  out: dx, which may be x, residual, dy or dsum."""
     import torch
     desc = _norm_call(x, weight, bias, 0.0)
     rows = x.numel() // x.shape[-1]
@@ -1148,7 +1148,8 @@ def agent_layer_norm_bwd(x, dy, saved, weight=None, bias=None, *, dsum=None, wan
     if "dw" in result or "db" in result:
         need = int(lib().agent_layer_norm_bwd_workspace_bytes(ctypes.byref(desc)))
         workspace = _ffn_workspace(need, workspace, stream, x.device)
-    st = lib().agent_layer_norm_bwd(ctypes.byref(desc), _norm_rows("x", x, x), _norm_rows("dy", dy, x), saved.data_ptr(), _ptr(weight),
+    st = lib().agent_layer_norm_bwd(ctypes.byref(desc), _norm_rows("x", x, x), _norm_rows("residual", residual, x),
+                                    _norm_rows("dy", dy, x), saved.data_ptr(), _ptr(weight),
                                     _norm_rows("dsum", dsum, x), _ptr(workspace),
                                     0 if workspace is None else workspace.numel() * workspace.element_size(),
                                     _norm_rows("dx", result.get("dx"), x), _ptr(result.get("dw")), _ptr(result.get("db")),

@@ -93,27 +93,28 @@ aa_status agent_layer_norm_fwd(const aa_layer_norm* desc, const aa_rows* x, cons
   return launch(desc, a, false, nullptr, nullptr, hip_stream);
 }
 
-aa_status agent_layer_norm_bwd(const aa_layer_norm* desc, const aa_rows* x, const aa_rows* dy, const float* saved, const void* weight,
-                               const aa_rows* dsum, void* workspace, size_t workspace_bytes, const aa_rows* dx, void* dweight,
+aa_status agent_layer_norm_bwd(const aa_layer_norm* desc, const aa_rows* x, const aa_rows* residual, const aa_rows* dy, const float* saved,
+                               const void* weight, const aa_rows* dsum, void* workspace, size_t workspace_bytes, const aa_rows* dx, void* dweight,
                                void* dbias, void* hip_stream) {
   aa_status st = check_desc(desc);
   if (st != AA_OK) return st;
   if (!saved) return AA_ERR_NULL;
   NormArgs a = args_of(desc);
-  Range in[3], out;
+  Range in[4], out;
   if ((st = take(desc, x, true, &in[0], &a.x)) != AA_OK) return st;
   if ((st = take(desc, dy, true, &in[1], &a.dy)) != AA_OK) return st;
   if ((st = take(desc, dsum, false, &in[2], &a.dsum)) != AA_OK) return st;
+  if ((st = take(desc, residual, false, &in[3], &a.r)) != AA_OK) return st;
   if ((st = take(desc, dx, false, &out, &a.dx)) != AA_OK) return st;
   const size_t es = elem_bytes(desc), ws = desc->weight_dtype == AA_F32 ? 4 : 2;
-  for (const Range& r : {in[0], in[1], in[2], out})
+  for (const Range& r : {in[0], in[1], in[2], in[3], out})
     if ((uintptr_t)r.p % es) return AA_ERR_SHAPE;
   if ((uintptr_t)weight % ws || (uintptr_t)dweight % ws || (uintptr_t)dbias % ws || (uintptr_t)saved % 8) return AA_ERR_SHAPE;
   const bool sums = dweight || dbias;
   const size_t need = sums ? agent_layer_norm_bwd_workspace_bytes(desc) : 0;
   if (sums && (!workspace || ((uintptr_t)workspace % kAlign) != 0 || workspace_bytes < need)) return AA_ERR_WORKSPACE;
   const Range written[] = {{sums ? workspace : nullptr, need}, {dweight, weight_bytes(desc)}, {dbias, weight_bytes(desc)}};
-  const Range read[] = {in[0], in[1], in[2], {saved, (size_t)8 * desc->rows}, {weight, weight_bytes(desc)}};
+  const Range read[] = {in[0], in[1], in[2], in[3], {saved, (size_t)8 * desc->rows}, {weight, weight_bytes(desc)}};
   for (size_t i = 0; i < 3; ++i) {
     for (size_t j = 0; j < i; ++j)
       if (aa::meet(written[i], written[j])) return AA_ERR_ALIAS;
@@ -121,7 +122,7 @@ aa_status agent_layer_norm_bwd(const aa_layer_norm* desc, const aa_rows* x, cons
       if (aa::meet(written[i], r)) return AA_ERR_ALIAS;
     if (aa::meet(written[i], out)) return AA_ERR_ALIAS;
   }
-  for (const Range& r : read)      // dx may be the rows of x, dy or dsum
+  for (const Range& r : read)      // dx may be the rows of x, residual, dy or dsum
     if (aa::meet(out, r) && !(r.pitch != 0 && same(out, r))) return AA_ERR_ALIAS;
   if (!sums && !a.dx.data) return AA_OK;
   a.w = weight, a.stats = (float2*)const_cast<float*>(saved), a.partial = sums ? (float*)workspace : nullptr;

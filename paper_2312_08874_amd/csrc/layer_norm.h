@@ -16,7 +16,7 @@ struct NormRows {      // rows of a tensor: stride in elements
 };
 
 struct NormArgs {
-  NormRows x, r, y, sum;              // forward; backward: x is the normed sum
+  NormRows x, r, y, sum;              // r: none, where what is normed is x
   NormRows dy, dsum, dx;              // backward
   const void *w, *b;                  // in fp32 or the element type
   int wide_weights;                   // 1: fp32

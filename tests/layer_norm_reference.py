@@ -45,9 +45,9 @@ def forward(x, w, b, eps, residual=None):
     return {"y": rounded(y, dy, x.dtype), "sum": rounded(s, ds, x.dtype), "h": (h, dh), "r": (r, rel), "mean": (mean, dmean)}
 
 
-def backward(s, dy, w, b, eps, dsum=None):
-    """From the normed rows s as they are."""
-    f = forward(s, None, None, eps)
+def backward(s, dy, w, b, eps, dsum=None, residual=None):
+    """From the normed rows s (+ residual) as they are."""
+    f = forward(s, None, None, eps, residual)
     (h, dh), (r, rel) = f["h"], f["r"]
     C, R = s.shape[-1], s.numel() // s.shape[-1]
     d = dy.double().cpu()

@@ -89,6 +89,12 @@ def test_norm_and_its_gradients(case):
     assert set(grads) == set(expected)
     for name in grads:
         close(grads[name], expected[name], name)
+    if r is not None:      # from the sum as it was normed, unrounded
+        saved = rest[-1]
+        both = binding.agent_layer_norm_bwd(x, dy, saved, w, b, residual=r, dsum=ds)
+        expected = ref.backward(x, dy, w, b, eps, ds, residual=r)
+        for name in both:
+            close(both[name], expected[name], name)
     more = binding.agent_layer_norm_bwd(s, dy, stats, w, b, dsum=ds)
     assert all(torch.equal(grads[n], more[n]) for n in grads)
     alone = binding.agent_layer_norm_fwd(x, w, b, residual=r, eps=eps)
