@@ -50,7 +50,7 @@ NormArgs args_of(const aa_layer_norm* d) {
 }
 
 aa_status launch(const aa_layer_norm* d, NormArgs& a, bool back, void* dw, void* db, void* stream) {
-  const aa::NormShape s = aa::norm_shape(elem_bytes(d), d->width);
+  const aa::NormShape s = aa::norm_shape(elem_bytes(d), d->width, back);
   a.blocks = aa::norm_blocks(s, d->rows, back);
   const auto fn = d->dtype == AA_F32 ? aa::launch_layer_norm_f32 : d->dtype == AA_F16 ? aa::launch_layer_norm_f16 : aa::launch_layer_norm_bf16;
   return fn(a, s, back, dw, db, (hipStream_t)stream) == hipSuccess ? AA_OK : AA_ERR_HIP;
@@ -62,7 +62,7 @@ extern "C" {
 
 size_t agent_layer_norm_bwd_workspace_bytes(const aa_layer_norm* desc) {
   if (check_desc(desc) != AA_OK) return 0;
-  const int blocks = aa::norm_blocks(aa::norm_shape(elem_bytes(desc), desc->width), desc->rows, true);
+  const int blocks = aa::norm_blocks(aa::norm_shape(elem_bytes(desc), desc->width, true), desc->rows, true);
   return ((size_t)blocks * 2 * desc->width * 4 + kAlign - 1) / kAlign * kAlign;
 }
 
