@@ -17,6 +17,8 @@ constexpr int kLowKeys = 512;
 
 struct SoftmaxArgs {
   TokenView q, k, v, out, dout, dq, dk, dv;
+  TokenView dout_whole;      // fp32, whose q, k, v and dout are taken apart into terms
+  unsigned term;             // bytes from a row's one term to the next
   // what the forward pass keeps, null: nothing: lse (natural logarithm) [batch][heads_q][tokens_q] and, of 16-bit types, what
   // rounding took from out, [..][d], itself in the type
   float* lse;
@@ -39,8 +41,13 @@ struct SoftmaxArgs {
   int first_batch;      // of a launch that sums them
 };
 
-// Width that the kernels are compiled for: a multiple of the matrix instruction's 32 rows.
-inline int softmax_width(int d) { return d <= 32 ? 32 : d <= 64 ? 64 : d <= 96 ? 96 : d <= 128 ? 128 : 256; }
+// Width that the kernels are compiled for: channels of the scores' products, in steps of 16; results are taken in tiles of 32.
+inline int softmax_width(int d) {
+  for (const int w : {32, 48, 64, 80, 96, 128})
+    if (d <= w) return w;
+  return 256;
+}
+constexpr int softmax_tiles_across(int dp) { return (dp + 31) / 32; }
 
 // Tiles of `rows` tokens along the queries (or keys) of all sequences together; sequence s of a packed run has the tiles from
 // starts[s] / rows + s on, which leaves each at least the tiles it needs, whatever the lengths on the device are.
@@ -49,7 +56,11 @@ inline long long softmax_tiles(int tokens, int batch, int sequences, int rows) {
 }
 
 // A tile of keys (or of queries, for the keys' kernel) on its way through LDS, and the tokens that a block's waves take side by side.
-constexpr int softmax_step(int es) { return es == 4 ? 32 : 64; }
+// dp: width that the kernels are compiled for
+constexpr int softmax_step(int es, int dp) { return es == 4 && dp > 32 ? 32 : 64; }
+// Terms that an operand is taken apart into by all kernels but that of few queries, which reads keys and values once and is bound by that:
+// three bf16 terms for fp32, up to where two tiles of them fit in LDS.
+constexpr int softmax_terms(int es, int dp) { return es == 4 && dp <= 128 ? 3 : 1; }
 // Waves of a columns block: as many as 160 KB of LDS hold two tiles of 32 keys of.
 constexpr int softmax_column_waves(int es, int dp) { return es * dp <= 256 ? 4 : es * dp <= 512 ? 2 : 1; }
 
@@ -62,6 +73,9 @@ inline int softmax_waves(int tokens, int batch, int sequences, int heads, int mo
     const long long blocks = softmax_tiles(tokens, batch, sequences, 32 * waves) * heads;
     return (blocks + kSoftmaxUnits - 1) / kSoftmaxUnits * waves;
   };
+#ifdef FW
+  return FW;
+#endif
   const int waves = rounds(2) < rounds(4) ? 2 : 4;
   return most >= 8 && rounds(8) <= rounds(waves) ? 8 : waves;
 }
@@ -87,7 +101,7 @@ inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a, int es) {
   const long long queries = softmax_typical(a.tokens_q, a.sequences), keys = softmax_typical(a.tokens_k, a.sequences);
   p.waves = softmax_waves(a.tokens_q, a.batch, a.sequences, a.heads_q, softmax_most_waves(es, a.d));
   const long long row_blocks = softmax_tiles(a.tokens_q, a.batch, a.sequences, 128) * a.heads_q;
-  p.columns = queries <= 32 || row_blocks < kSoftmaxUnits;
+  p.columns = queries <= 16 || (row_blocks < kSoftmaxUnits && keys >= (es == 4 ? 512 : 1536));
   p.pack = 1, p.tile_tokens = 32 * p.waves, p.splits = 1;
   if (p.columns) {
     // heads that share keys side by side, where the tokens leave room

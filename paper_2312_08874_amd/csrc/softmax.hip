@@ -1,6 +1,6 @@
 // Softmax attention: launch sequences, and copies of tensors whose rows are no whole 16-byte pieces.
-#include "common.h"
 #include "kernels.h"
+#include "softmax_common.inc"
 
 namespace aa {
 
@@ -23,6 +23,45 @@ __global__ __launch_bounds__(256) void softmax_copy_kernel(TokenView from, T* to
     to[at] = c < d ? reinterpret_cast<const T*>(from.data)[b * from.sb + h * from.sh + i * from.sn + c] : (T)0;
   }
 }
+// fp32 rows to dense rows of three terms, 8 * pieces bf16 values each: eight channels a thread; along y the tensors
+struct TermsOf {
+  TokenView from;
+  uint16_t* to;
+  int heads, tokens;
+  unsigned count;      // threads
+};
+struct TermsArgs {
+  TermsOf t[4];
+  int d, pieces;
+};
+__global__ __launch_bounds__(256) void softmax_terms_kernel(TermsArgs a) {
+  const TermsOf& x = a.t[blockIdx.y];
+  const bool whole = a.d % 8 == 0 && ((uintptr_t)x.from.data | (x.from.sb | x.from.sh | x.from.sn) * 4) % 16 == 0;
+  for (unsigned at = 256 * blockIdx.x + threadIdx.x; at < x.count; at += 256 * gridDim.x) {
+    const unsigned row = at / (unsigned)a.pieces, c = 8 * (at - row * a.pieces);
+    const unsigned unit = row / (unsigned)x.tokens, i = row - unit * x.tokens, b = unit / (unsigned)x.heads, h = unit - b * x.heads;
+    const float* p = reinterpret_cast<const float*>(x.from.data) + b * x.from.sb + h * x.from.sh + i * x.from.sn + c;
+    float v[8];
+    if (whole) {
+      const f32x4 lo = *reinterpret_cast<const f32x4*>(p), hi = *reinterpret_cast<const f32x4*>(p + 4);
+#pragma unroll
+      for (int n = 0; n < 4; ++n) v[n] = lo[n], v[4 + n] = hi[n];
+    } else {
+#pragma unroll
+      for (int n = 0; n < 8; ++n) v[n] = (int)c + n < a.d ? p[n] : 0.0f;
+    }
+    u32x4 t[3];
+#pragma unroll
+    for (int n = 0; n < 4; ++n) {
+      uint32_t w[3];
+      three_terms(v[2 * n], v[2 * n + 1], w);
+#pragma unroll
+      for (int k = 0; k < 3; ++k) t[k][n] = w[k];
+    }
+#pragma unroll
+    for (int k = 0; k < 3; ++k) *reinterpret_cast<u32x4*>(x.to + (3ull * row + k) * 8 * a.pieces + c) = t[k];
+  }
+}
 
 int padded(int d, int es) { return (d * es + 15) / 16 * 16 / es; }
 
@@ -32,13 +71,15 @@ bool in_pieces(const TokenView& v, int batch, int heads, int tokens, int d, int 
   return d * es % 16 == 0 && (uintptr_t)v.data % 16 == 0 && strides * es % 16 == 0 && (tokens == 1 || v.sn * es < (1 << 24));
 }
 
-size_t copy_bytes(const TokenView& v, int batch, int heads, int tokens, int d, int es) {
+// terms > 1: taken apart in any case
+size_t copy_bytes(const TokenView& v, int batch, int heads, int tokens, int d, int es, int terms) {
+  if (terms > 1) return aligned((size_t)batch * heads * tokens * padded(d, 2) * 2 * terms);
   if (v.data != nullptr && in_pieces(v, batch, heads, tokens, d, es)) return 0;
   return aligned((size_t)batch * heads * tokens * padded(d, es) * es);
 }
 
 hipError_t copy_to(TokenView& v, char*& ws, int batch, int heads, int tokens, int d, int es, hipStream_t st) {
-  const size_t bytes = copy_bytes(v, batch, heads, tokens, d, es);
+  const size_t bytes = copy_bytes(v, batch, heads, tokens, d, es, 1);
   if (bytes == 0) return hipSuccess;
   const int width = padded(d, es);
   const long long count = (long long)batch * heads * tokens * width;
@@ -48,6 +89,35 @@ hipError_t copy_to(TokenView& v, char*& ws, int batch, int heads, int tokens, in
   v = TokenView{ws, (long long)heads * tokens * width, (long long)tokens * width, width};
   ws += bytes;
   return hipGetLastError();
+}
+
+// q, k, v and, of the backward pass, dout in a form that the kernels can take, in the workspace where they lie in none
+hipError_t take_inputs(SoftmaxArgs& a, char*& ws, int es, int terms, bool back, hipStream_t st) {
+  TokenView* const views[] = {&a.q, &a.k, &a.v, &a.dout};
+  const int count = back ? 4 : 3;
+  a.term = 2 * padded(a.d, 2);
+  if (terms > 1) {
+    TermsArgs t{};
+    t.d = a.d, t.pieces = padded(a.d, 2) / 8;
+    unsigned most = 0;
+    for (int i = 0; i < count; ++i) {
+      const bool keys = i == 1 || i == 2;
+      const int heads = keys ? a.heads_k : a.heads_q, tokens = keys ? a.tokens_k : a.tokens_q;
+      const long long step = terms * padded(a.d, 2), rows = (long long)a.batch * heads * tokens;
+      t.t[i] = TermsOf{*views[i], (uint16_t*)ws, heads, tokens, (unsigned)(rows * t.pieces)};
+      most = std::max(most, t.t[i].count);
+      *views[i] = TokenView{ws, heads * tokens * step, tokens * step, step};
+      ws += copy_bytes(*views[i], a.batch, heads, tokens, a.d, es, terms);
+    }
+    softmax_terms_kernel<<<dim3(std::min((most + 255) / 256, 1u << 13), (unsigned)count), 256, 0, st>>>(t);
+    return hipGetLastError();
+  }
+  for (int i = 0; i < count; ++i) {
+    const bool keys = i == 1 || i == 2;
+    const hipError_t err = copy_to(*views[i], ws, a.batch, keys ? a.heads_k : a.heads_q, keys ? a.tokens_k : a.tokens_q, a.d, es, st);
+    if (err != hipSuccess) return err;
+  }
+  return hipSuccess;
 }
 
 hipError_t launch(int dtype, const SoftmaxArgs& a, SoftmaxPass pass, long long tiles, hipStream_t st) {
@@ -71,6 +141,8 @@ bool softmax_fits(int dtype, const SoftmaxArgs& a) {      // blocks are numbered
   const SoftmaxPlan p = softmax_plan(a, es);
   const SoftmaxBackPlan q = softmax_back_plan(a, es, false), k = softmax_back_plan(a, es, true);
   const long long outer = a.sequences > 0 ? 1 : a.batch, lim = 1ll << 30;
+  // and so are the pieces of eight channels that fp32 tensors are taken apart in
+  if (es == 4 && std::max(query_rows(a), key_rows(a)) * (padded(a.d, 2) / 8) >= 2 * lim) return false;
   return p.tiles * outer * a.heads_q / p.pack * p.splits < lim && q.tiles * outer * a.heads_q * q.splits < lim &&
          k.tiles * outer * a.heads_k * k.splits < lim;
 }
@@ -82,22 +154,22 @@ size_t softmax_saved_bytes(int dtype, const SoftmaxArgs& a) {
 
 size_t softmax_fwd_workspace(int dtype, const SoftmaxArgs& a) {
   const int es = dtype == 0 ? 4 : 2;
-  size_t bytes = copy_bytes(a.q, a.batch, a.heads_q, a.tokens_q, a.d, es) + copy_bytes(a.k, a.batch, a.heads_k, a.tokens_k, a.d, es) +
-                 copy_bytes(a.v, a.batch, a.heads_k, a.tokens_k, a.d, es);
   const SoftmaxPlan p = softmax_plan(a, es);
+  const int terms = p.columns ? 1 : softmax_terms(es, softmax_width(a.d));
+  size_t bytes = copy_bytes(a.q, a.batch, a.heads_q, a.tokens_q, a.d, es, terms) + copy_bytes(a.k, a.batch, a.heads_k, a.tokens_k, a.d, es, terms) +
+                 copy_bytes(a.v, a.batch, a.heads_k, a.tokens_k, a.d, es, terms);
   if (p.splits > 1) bytes += aligned((size_t)p.splits * query_rows(a) * a.d * 4) + aligned((size_t)p.splits * query_rows(a) * 8);
   return bytes;
 }
 
 hipError_t launch_softmax_fwd(int dtype, SoftmaxArgs a, void* workspace, hipStream_t st) {
   const int es = dtype == 0 ? 4 : 2;
+  const SoftmaxPlan p = softmax_plan(a, es);
+  const int terms = p.columns ? 1 : softmax_terms(es, softmax_width(a.d));
   char* ws = (char*)workspace;
   a.wide = wide_result(a.out, a.batch, a.heads_q, a.tokens_q, a.d, es);
-  hipError_t err = copy_to(a.q, ws, a.batch, a.heads_q, a.tokens_q, a.d, es, st);
-  if (err == hipSuccess) err = copy_to(a.k, ws, a.batch, a.heads_k, a.tokens_k, a.d, es, st);
-  if (err == hipSuccess) err = copy_to(a.v, ws, a.batch, a.heads_k, a.tokens_k, a.d, es, st);
+  hipError_t err = take_inputs(a, ws, es, terms, false, st);
   if (err != hipSuccess) return err;
-  const SoftmaxPlan p = softmax_plan(a, es);
   a.waves = p.waves, a.pack = p.pack, a.tile_tokens = p.tile_tokens, a.splits = p.splits;
   if (p.splits > 1) {
     a.part = (float*)ws;
@@ -108,9 +180,9 @@ hipError_t launch_softmax_fwd(int dtype, SoftmaxArgs a, void* workspace, hipStre
 }
 
 size_t softmax_bwd_workspace(int dtype, const SoftmaxArgs& a) {
-  const int es = dtype == 0 ? 4 : 2;
-  const size_t q = copy_bytes(a.q, a.batch, a.heads_q, a.tokens_q, a.d, es), k = copy_bytes(a.k, a.batch, a.heads_k, a.tokens_k, a.d, es),
-               v = copy_bytes(a.v, a.batch, a.heads_k, a.tokens_k, a.d, es), g = copy_bytes(a.dout, a.batch, a.heads_q, a.tokens_q, a.d, es);
+  const int es = dtype == 0 ? 4 : 2, terms = softmax_terms(es, softmax_width(a.d));
+  const size_t q = copy_bytes(a.q, a.batch, a.heads_q, a.tokens_q, a.d, es, terms), k = copy_bytes(a.k, a.batch, a.heads_k, a.tokens_k, a.d, es, terms),
+               v = copy_bytes(a.v, a.batch, a.heads_k, a.tokens_k, a.d, es, terms), g = copy_bytes(a.dout, a.batch, a.heads_q, a.tokens_q, a.d, es, terms);
   const int sq = softmax_back_plan(a, es, false).splits, sk = softmax_back_plan(a, es, true).splits;
   // the queries' parts are added up before the keys' are written
   const size_t parts = std::max(sq > 1 ? aligned((size_t)sq * query_rows(a) * a.d * 4) : 0,
@@ -119,17 +191,15 @@ size_t softmax_bwd_workspace(int dtype, const SoftmaxArgs& a) {
 }
 
 hipError_t launch_softmax_bwd(int dtype, SoftmaxArgs a, void* workspace, hipStream_t st) {
-  const int es = dtype == 0 ? 4 : 2;
+  const int es = dtype == 0 ? 4 : 2, terms = softmax_terms(es, softmax_width(a.d));
   char* ws = (char*)workspace;
+  a.dout_whole = a.dout;
   a.peaks = (unsigned*)ws, ws += kAlign;
   a.stats = (float*)ws, ws += aligned((size_t)query_rows(a) * 8);
   a.wide = 1;
-  for (const TokenView* v : {&a.out, &a.dq}) a.wide = a.wide && wide_result(*v, a.batch, a.heads_q, a.tokens_q, a.d, es);
+  for (const TokenView* v : {&a.out, &a.dq, &a.dout_whole}) a.wide = a.wide && wide_result(*v, a.batch, a.heads_q, a.tokens_q, a.d, es);
   for (const TokenView* v : {&a.dk, &a.dv}) a.wide = a.wide && wide_result(*v, a.batch, a.heads_k, a.tokens_k, a.d, es);
-  hipError_t err = copy_to(a.q, ws, a.batch, a.heads_q, a.tokens_q, a.d, es, st);
-  if (err == hipSuccess) err = copy_to(a.k, ws, a.batch, a.heads_k, a.tokens_k, a.d, es, st);
-  if (err == hipSuccess) err = copy_to(a.v, ws, a.batch, a.heads_k, a.tokens_k, a.d, es, st);
-  if (err == hipSuccess) err = copy_to(a.dout, ws, a.batch, a.heads_q, a.tokens_q, a.d, es, st);
+  hipError_t err = take_inputs(a, ws, es, terms, true, st);
   if (err == hipSuccess && dtype == 1) err = launch(dtype, a, SoftmaxPass::kPeaks, 0, st);
   if (err != hipSuccess) return err;
   const SoftmaxBackPlan q = softmax_back_plan(a, es, false), k = softmax_back_plan(a, es, true);
