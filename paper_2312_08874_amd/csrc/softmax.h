@@ -68,15 +68,12 @@ constexpr int kSoftmaxUnits = 256;      // compute units
 
 // Waves of a block of rows, 32 rows each: MEASURED
 constexpr int softmax_most_waves(int es, int d) { return es == 2 && d > 32 && d <= 128 ? 8 : 4; }
-inline int softmax_waves(int tokens, int batch, int sequences, int heads, int most) {
+inline int softmax_waves(int tokens, int batch, int sequences, int heads, int most, int terms) {
   auto rounds = [&](int waves) {
     const long long blocks = softmax_tiles(tokens, batch, sequences, 32 * waves) * heads;
     return (blocks + kSoftmaxUnits - 1) / kSoftmaxUnits * waves;
   };
-#ifdef FW
-  return FW;
-#endif
-  const int waves = rounds(2) < rounds(4) ? 2 : 4;
+  const int waves = rounds(2) * (terms > 1 ? 3 : 2) < rounds(4) * 2 ? 2 : 4;
   return most >= 8 && rounds(8) <= rounds(waves) ? 8 : waves;
 }
 
@@ -99,7 +96,7 @@ inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a, int es) {
   SoftmaxPlan p{};
   const int group = a.heads_q / a.heads_k, outer = a.sequences > 0 ? 1 : a.batch;
   const long long queries = softmax_typical(a.tokens_q, a.sequences), keys = softmax_typical(a.tokens_k, a.sequences);
-  p.waves = softmax_waves(a.tokens_q, a.batch, a.sequences, a.heads_q, softmax_most_waves(es, a.d));
+  p.waves = softmax_waves(a.tokens_q, a.batch, a.sequences, a.heads_q, softmax_most_waves(es, a.d), softmax_terms(es, softmax_width(a.d)));
   const long long row_blocks = softmax_tiles(a.tokens_q, a.batch, a.sequences, 128) * a.heads_q;
   p.columns = queries <= 16 || (row_blocks < kSoftmaxUnits && keys >= (es == 4 ? 512 : 1536));
   p.pack = 1, p.tile_tokens = 32 * p.waves, p.splits = 1;
@@ -127,10 +124,14 @@ struct SoftmaxBackPlan {
 inline SoftmaxBackPlan softmax_back_plan(const SoftmaxArgs& a, int es, bool keys) {
   const int tokens = keys ? a.tokens_k : a.tokens_q, heads = keys ? a.heads_k : a.heads_q;
   SoftmaxBackPlan p;
-  p.waves = softmax_waves(tokens, a.batch, a.sequences, heads, keys ? 4 : softmax_most_waves(es, a.d));
+  p.waves = softmax_waves(tokens, a.batch, a.sequences, heads, keys ? 4 : softmax_most_waves(es, a.d), softmax_terms(es, softmax_width(a.d)));
   p.tiles = softmax_tiles(tokens, 1, a.sequences, 32 * p.waves);
-  p.splits = softmax_splits(p.tiles * (a.sequences > 0 ? 1 : a.batch) * heads, 2 * kSoftmaxUnits,
-                            keys ? softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k) : softmax_typical(a.tokens_k, a.sequences), 512);
+  const long long across = keys ? softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k) : softmax_typical(a.tokens_k, a.sequences);
+  // Blocks for each compute unit that ranges are to make up for.  Uneven ones (causal) are shared out better where there are more, which
+  // costs their parts' way through memory: the keys' kernel of 2 x 4096 tokens, 16 heads on 4 of 128, and its sum take 383 us with two
+  // ranges, 315 with three, 328 with four; of 2 x 2000 tokens, 8 heads of 80, a step takes 229 with two and 247 with three.
+  const int each = keys ? (a.causal && across >= 8192 ? 3 : 2) : a.causal ? 2 : 1;
+  p.splits = softmax_splits(p.tiles * (a.sequences > 0 ? 1 : a.batch) * heads, each * kSoftmaxUnits, across, 512);
   return p;
 }
 
