@@ -240,10 +240,8 @@ def _own(state):
     binding = state["binding"]
     if case["kind"] == "norm_train":
         y, *total, saved = binding.agent_layer_norm_fwd(s["x"], s.get("w"), s.get("b"), residual=s.get("r"), eps=EPS, save=True)
-        # from the sum, or where gradients in 32 bits would show its rounding, from what it is the sum of
-        whole = s["w"].dtype == torch.float32 if "w" in s else not total
-        g = binding.agent_layer_norm_bwd(s["x"] if whole or not total else total[0], s["dy"], saved, s.get("w"), s.get("b"),
-                                         residual=s.get("r") if whole else None, dsum=s.get("dsum"))
+        # from what the sum is of: its rounding would show in the weights' gradients
+        g = binding.agent_layer_norm_bwd(s["x"], s["dy"], saved, s.get("w"), s.get("b"), residual=s.get("r"), dsum=s.get("dsum"))
         return {"y": y, **({"sum": total[0]} if total else {}), **g}
     mixed = state["mixed"]
     out, lse = binding.agent_softmax_attn_fwd(s["q"], s["k"], s["v"], causal=case["causal"], save=True, **mixed)
