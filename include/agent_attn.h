@@ -424,8 +424,10 @@ aa_status agent_gated_ffn_bwd(const aa_ffn *desc, const void *x, const aa_ffn_we
  *           [sequences + 1], rising, within tokens_q and tokens_k) are sequence s, which may be empty
  * Rows of no sequence are not used, whatever they hold, and as results stay as they were.  Lengths and starts are read on the
  * device and kept within the tensors' rows there; starts that fall give results of no meaning.
- * Scores and sums are fp32; p (and, backward, ds) is rounded to dtype, as an operand; results are rounded once.  A NaN or
- * infinity in a row of a sequence may show in every result of that head's sequence.  d <= 256. */
+ * Scores and sums are fp32; p (and, backward, ds) is rounded to dtype, as an operand (fp32: products are taken of three bf16
+ * terms of either operand, to 2^-24 of the largest, up to d 128 and for more than few queries); results are rounded once.  fp16: ds is held
+ * in steps of 2^-37 of the product of the call's longest rows of dout and v, which much smaller gradients beside it lose digits to.
+ * A NaN or infinity in a row of a sequence may show in every result of that head's sequence.  d <= 256. */
 typedef struct {
   int32_t batch, heads_q, heads_k; /* heads_q a multiple of heads_k */
   int32_t tokens_q, tokens_k;      /* rows of q, out and of k, v */
@@ -437,8 +439,9 @@ typedef struct {
   float scale;                     /* 0: d^-1/2 */
 } aa_softmax_attn;
 
-/* Bytes of what the forward pass keeps, and of device workspace of either pass, which may be 0 for the forward pass.  Tensors whose rows are no whole, aligned 16-byte
- * pieces are copied there first; a view that is NULL counts as one of them.  0 for an invalid descriptor. */
+/* Bytes of what the forward pass keeps, and of device workspace of either pass, which may be 0 for the forward pass.  Tensors whose rows
+ * are no whole, aligned 16-byte pieces less than 16 MiB apart are copied there first (fp32 in most calls: as its terms); a view that is NULL
+ * counts as one of them.  0 for an invalid descriptor. */
 size_t agent_softmax_attn_saved_bytes(const aa_softmax_attn *desc);
 size_t agent_softmax_attn_workspace_bytes(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v);
 size_t agent_softmax_attn_bwd_workspace_bytes(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
@@ -468,7 +471,8 @@ typedef struct {
 /* Layer norm of every row, with the residual sum before it in the same pass (host struct):
  *   s = x + residual,  h = (s - mean s) r,  r = (mean of (s - mean s)^2 + eps)^-1/2,  y = h weight + bias
  * Sums are fp32, the mean is taken off before the squares are summed; s is normed unrounded.  weight, bias: device, dense
- * [width], in fp32 or dtype; NULL: ones, zeros.  width <= 32768.  A row of equal values with eps 0 has no norm (NaN). */
+ * [width], in fp32 or dtype; NULL: ones, zeros.  width <= 32768.  A row of equal values with eps 0 has
+ * no norm (NaN, or what the rounding of its mean leaves). */
 typedef struct {
   int32_t rows, width;
   int32_t dtype, weight_dtype; /* aa_dtype of the rows; of weight and bias: AA_F32 or dtype */

@@ -1122,7 +1122,8 @@ def agent_layer_norm_fwd(x, weight=None, bias=None, *, residual=None, eps=1e-5, 
         sum_out = _dense_like(x, stream)
     saved = None
     if save:
-        saved = _alloc_bytes(8 * (x.numel() // x.shape[-1]), stream, x.device).view(torch.float32).view(*x.shape[:-1], 2)
+        with torch.cuda.stream(stream):      # None: the current one
+            saved = torch.empty((x.numel() // x.shape[-1], 2), dtype=torch.float32, device=x.device)
     _check(lib().agent_layer_norm_fwd(*_layer_norm_args(x, weight, bias, residual, eps, saved, out, sum_out, stream)), "agent_layer_norm_fwd")
     results = (out,) + (() if sum_out is None else (sum_out,)) + ((saved,) if save else ())
     return results if len(results) > 1 else out
@@ -1132,8 +1133,9 @@ def agent_layer_norm_fwd(x, weight=None, bias=None, *, residual=None, eps=1e-5, 
 def agent_layer_norm_bwd(x, dy, saved, weight=None, bias=None, *, residual=None, dsum=None, want_dx=True, want_weight_grads=True,
                          out=None, workspace=None, stream=None):
     """Gradients of agent_layer_norm_fwd for the gradient dy of its y; x and residual: as in the forward pass, or x: its rounded
-    sum (which leaves dw with the error of that rounding), saved: what it returned, dsum: a gradient of s from elsewhere, which is added.  A dict of dx (the gradient of x and of residual) and, for
-    the weights present and want_weight_grads, dw and db in their type.  out: dx, which may be x, residual, dy or dsum."""
+    sum (which leaves dw with the error of that rounding), saved: what it returned, dsum: a gradient of s from elsewhere, which is
+    added.  A dict of dx (the gradient of x and of residual) and, for the weights present and want_weight_grads, dw and db in
+    their type.  out: dx, which may be x, residual, dy or dsum."""
     import torch
     desc = _norm_call(x, weight, bias, 0.0)
     rows = x.numel() // x.shape[-1]

@@ -4,10 +4,13 @@
     y = x + (agent attention of q, k, v) Wout^T + bout
     z = y + gated feed-forward block of rms(y) w2
 
-Matrix products and the norms over the whole width are torch's; everything between them is one call of the library, and
+With attention="softmax" every token attends to every other instead, as the late stages of the paper's models do; with norm="layer"
+layer norms with biases stand for the norms by the root mean square, the second in one pass with the sum y.  Matrix products and
+the norms by the root mean square over the whole width are torch's; everything between them is one call of the library, and
 torch.autograd.Function ties its backward pass to autograd, once: a second derivative through them is an error.
 
     python -m paper_2312_08874_amd.block [--dtype bf16] [--batch 8] [--side 32] [--width 512] [--heads 8] [--steps 20]
+                                         [--attention softmax] [--norm layer]
 
 trains one block on synthetic data (its output is to reproduce a fixed random linear map of its input) and prints the loss.
 """
@@ -22,7 +25,7 @@ from . import binding
 
 
 class _Attention(torch.autograd.Function):
-    """The fused projection's output [B,T,3,H,d] -> [B,T,H,d]: norm and rotation of q and k, then agent attention."""
+    """The fused projection's output [B,T,3,H,d] -> [B,T,H,d]: norm and rotation of q and k, then the attention (grids None: softmax)."""
 
     @staticmethod
     def forward(ctx, qkv, w_q, w_k, rope, eps, grids):
@@ -32,23 +35,49 @@ class _Attention(torch.autograd.Function):
         tq, tk, tv = (t.permute(0, 2, 1, 3) for t in turned.unbind(2))
         binding.agent_qk_norm_fwd(q, k, rope, weights=(w_q, w_k), eps=eps, out=(tq, tk))
         out = torch.empty_like(qkv[:, :, 0], memory_format=torch.contiguous_format)
-        binding.agent_attn_fwd(tq, tk, tv, out=out.permute(0, 2, 1, 3), **grids)
-        ctx.save_for_backward(qkv, w_q, w_k, turned)
+        if grids is None:
+            _, saved = binding.agent_softmax_attn_fwd(tq, tk, tv, save=True, out=out.permute(0, 2, 1, 3))
+            ctx.save_for_backward(qkv, w_q, w_k, turned, out, saved)
+        else:
+            binding.agent_attn_fwd(tq, tk, tv, out=out.permute(0, 2, 1, 3), **grids)
+            ctx.save_for_backward(qkv, w_q, w_k, turned)
         ctx.rope, ctx.eps, ctx.grids = rope, eps, grids
         return out
 
     @staticmethod
     @once_differentiable
     def backward(ctx, d_out):
-        qkv, w_q, w_k, turned = ctx.saved_tensors
+        qkv, w_q, w_k, turned, *kept = ctx.saved_tensors
         q, k, _ = (t.permute(0, 2, 1, 3) for t in qkv.unbind(2))
         tq, tk, tv = (t.permute(0, 2, 1, 3) for t in turned.unbind(2))
-        g = binding.agent_attn_bwd(tq, tk, tv, d_out.contiguous().permute(0, 2, 1, 3), **ctx.grids)
+        d_out = d_out.contiguous().permute(0, 2, 1, 3)
         d_qkv = torch.empty_like(qkv)
         dq, dk, dv = (t.permute(0, 2, 1, 3) for t in d_qkv.unbind(2))
-        dv.copy_(g["dV"])
+        if ctx.grids is None:
+            out, saved = kept
+            g = binding.agent_softmax_attn_bwd(tq, tk, tv, out.permute(0, 2, 1, 3), saved, d_out, grads=(dq, dk, dv))
+        else:
+            g = binding.agent_attn_bwd(tq, tk, tv, d_out, **ctx.grids)
+            dv.copy_(g["dV"])
         w = binding.agent_qk_norm_bwd(q, k, g["dQ"], g["dK"], ctx.rope, weights=(w_q, w_k), eps=ctx.eps, out=(dq, dk))
         return d_qkv, w["dw_q"], w["dw_k"], None, None, None
+
+
+class _LayerNorm(torch.autograd.Function):
+    """Layer norm of x, or of x + residual, which is the second result."""
+
+    @staticmethod
+    def forward(ctx, x, residual, w, b, eps):
+        y, *total, saved = binding.agent_layer_norm_fwd(x, w, b, residual=residual, eps=eps, save=True)
+        ctx.save_for_backward(x, residual, w, b, saved)
+        return (y, *total) if total else y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, d_sum=None):
+        x, residual, w, b, saved = ctx.saved_tensors
+        g = binding.agent_layer_norm_bwd(x, dy.contiguous(), saved, w, b, residual=residual, dsum=None if d_sum is None else d_sum.contiguous())
+        return g["dx"], None if residual is None else g["dx"], g["dw"], g["db"], None
 
 
 class _FeedForward(torch.autograd.Function):
@@ -73,11 +102,14 @@ def _rms(x, w, eps):
 
 
 class AgentBlock(torch.nn.Module):
-    """x [B, T, width] -> [B, T, width]; T = the cells of `grid`.  hidden: of the feed-forward block (default 8/3 of the width)."""
+    """x [B, T, width] -> [B, T, width]; T = the cells of `grid`.  hidden: of the feed-forward block (default 8/3 of the width).
+    attention: "agent", or "softmax" (agent_grid may then be None); norm: "rms" or "layer"."""
 
-    def __init__(self, width, heads, grid, agent_grid, *, hidden=None, activation="silu", base=10000.0, eps=1e-6, dtype=torch.bfloat16,
-                 device="cuda", seed=0):
+    def __init__(self, width, heads, grid, agent_grid=None, *, hidden=None, activation="silu", base=10000.0, eps=1e-6, dtype=torch.bfloat16,
+                 device="cuda", seed=0, attention="agent", norm="rms"):
         super().__init__()
+        assert attention in ("agent", "softmax") and norm in ("rms", "layer"), "attention: agent or softmax; norm: rms or layer"
+        assert attention == "softmax" or agent_grid is not None, "agent attention needs the agents' grid"
         d, hidden = width // heads, hidden or width * 8 // 3
         assert width % heads == 0 and d % 4 == 0, "heads of a multiple of four channels"
         gen = torch.Generator(device=device).manual_seed(seed)
@@ -88,27 +120,46 @@ class AgentBlock(torch.nn.Module):
         def ones(n):
             return torch.nn.Parameter(torch.ones(n, device=device))
         self.heads, self.d, self.activation, self.eps = heads, d, activation, eps
-        self.grids = dict(grid=tuple(grid), agent_grid=tuple(agent_grid))
+        self.grids = None if attention == "softmax" else dict(grid=tuple(grid), agent_grid=tuple(agent_grid))
         self.rope = binding.Rope((d // 4, d // 4), grid=grid, base=base)
         self.w_qkv, self.w_out = weight(3 * width, width), weight(width, width)
         self.b_qkv = torch.nn.Parameter(torch.zeros(3 * width, device=device, dtype=dtype))
         self.b_out = torch.nn.Parameter(torch.zeros(width, device=device, dtype=dtype))
         self.w_gate, self.w_up, self.w_down = weight(hidden, width), weight(hidden, width), weight(width, hidden)
         self.norm1, self.norm2, self.norm_q, self.norm_k = ones(width), ones(width), ones(d), ones(d)
+        self.layer = norm == "layer"
+        if self.layer:
+            self.norm1_b, self.norm2_b = (torch.nn.Parameter(torch.zeros(width, device=device)) for _ in range(2))
+
+    def _norm(self, x, w, b, residual=None):
+        """Norm of x, or (norm, sum) of x + residual."""
+        if not self.layer:
+            if residual is None:
+                return _rms(x, w, self.eps)
+            total = residual + x
+            return _rms(total, w, self.eps), total
+        x, residual = x.contiguous(), None if residual is None else residual.contiguous()
+        if torch.is_grad_enabled():
+            return _LayerNorm.apply(x, residual, w, b, self.eps)
+        return binding.agent_layer_norm_fwd(x, w, b, residual=residual, eps=self.eps)
 
     def forward(self, x):
         B, T, C = x.shape
         training = torch.is_grad_enabled()
-        qkv = torch.nn.functional.linear(_rms(x, self.norm1, self.eps), self.w_qkv, self.b_qkv).view(B, T, 3, self.heads, self.d)
+        u = self._norm(x, self.norm1, self.norm1_b if self.layer else None)
+        qkv = torch.nn.functional.linear(u, self.w_qkv, self.b_qkv).view(B, T, 3, self.heads, self.d)
         if training:
             o = _Attention.apply(qkv, self.norm_q, self.norm_k, self.rope, self.eps, self.grids)
         else:      # q and k in place, where the projection wrote them
             q, k, v = (t.permute(0, 2, 1, 3) for t in qkv.unbind(2))
             binding.agent_qk_norm_fwd(q, k, self.rope, weights=(self.norm_q, self.norm_k), eps=self.eps, out=(q, k))
             o = torch.empty(B, T, self.heads, self.d, dtype=x.dtype, device=x.device)
-            binding.agent_attn_fwd(q, k, v, out=o.permute(0, 2, 1, 3), **self.grids)
-        y = x + torch.nn.functional.linear(o.view(B, T, C), self.w_out, self.b_out)
-        u = _rms(y, self.norm2, self.eps)
+            if self.grids is None:
+                binding.agent_softmax_attn_fwd(q, k, v, out=o.permute(0, 2, 1, 3))
+            else:
+                binding.agent_attn_fwd(q, k, v, out=o.permute(0, 2, 1, 3), **self.grids)
+        u, y = self._norm(torch.nn.functional.linear(o.view(B, T, C), self.w_out, self.b_out), self.norm2,
+                          self.norm2_b if self.layer else None, x)
         if training:
             return y + _FeedForward.apply(u, self.w_gate, self.w_up, self.w_down, self.activation)
         return y + binding.agent_gated_ffn_fwd(u, self.w_gate, self.w_up, self.w_down, activation=self.activation)
@@ -117,11 +168,13 @@ class AgentBlock(torch.nn.Module):
 def main():
     p = argparse.ArgumentParser(description="Trains one transformer block on synthetic data.")
     p.add_argument("--dtype", default="bf16", choices=("bf16", "f16", "f32"))
+    p.add_argument("--attention", default="agent", choices=("agent", "softmax"))
+    p.add_argument("--norm", default="rms", choices=("rms", "layer"))
     for name, value in (("batch", 8), ("side", 32), ("agents", 7), ("width", 512), ("heads", 8), ("steps", 20)):
         p.add_argument("--" + name, type=int, default=value)
     a = p.parse_args()
     dtype = {"bf16": torch.bfloat16, "f16": torch.float16, "f32": torch.float32}[a.dtype]
-    block = AgentBlock(a.width, a.heads, (a.side, a.side), (a.agents, a.agents), dtype=dtype)
+    block = AgentBlock(a.width, a.heads, (a.side, a.side), (a.agents, a.agents), dtype=dtype, attention=a.attention, norm=a.norm)
     gen = torch.Generator(device="cuda").manual_seed(1)
     x = torch.randn(a.batch, a.side * a.side, a.width, generator=gen, device="cuda").to(dtype)
     target = x.float() @ (torch.randn(a.width, a.width, generator=gen, device="cuda") / math.sqrt(a.width))

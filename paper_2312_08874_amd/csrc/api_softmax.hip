@@ -18,7 +18,7 @@ aa_status check_desc(const aa_softmax_attn* d) {
   if (d->dtype != AA_F32 && d->dtype != AA_F16 && d->dtype != AA_BF16) return AA_ERR_DTYPE;
   if (d->batch <= 0 || d->heads_q <= 0 || d->heads_k <= 0 || d->tokens_q <= 0 || d->tokens_k <= 0 || d->d <= 0) return AA_ERR_SHAPE;
   if (d->heads_q % d->heads_k != 0 || d->sequences < 0) return AA_ERR_SHAPE;
-  if (!(d->scale >= 0.0f) || !isfinite(d->scale)) return AA_ERR_SHAPE;
+  if (!(d->scale >= 0.0f) || !isfinite(d->scale * 1.4426950408889634f)) return AA_ERR_SHAPE;
   if (d->sequences > 0) {
     if (d->batch != 1 || d->lengths_q || d->lengths_k) return AA_ERR_SHAPE;
     if (!d->starts_q || !d->starts_k) return AA_ERR_NULL;

@@ -66,7 +66,10 @@ constexpr int softmax_column_waves(int es, int dp) { return es * dp <= 256 ? 4 :
 
 constexpr int kSoftmaxUnits = 256;      // compute units
 
-// Waves of a block of rows, 32 rows each: MEASURED
+// Waves of a block of rows, 32 rows each: as few rounds of blocks over the compute units as may be, two waves where four would be half
+// empty, eight, which share every tile of keys, where they cost no round.  Measured: windows of 49 tokens, 2048 x 12 heads, 79 us with two
+// and 96 with four; 37 packed images of 8192 tokens in all, a training step, 101 and 110; 128 x 128 tokens, 2359 with eight (forward and
+// for dq), 2432 with four, 2912 with two.  Terms take three times the LDS: two waves then cost more.
 constexpr int softmax_most_waves(int es, int d) { return es == 2 && d > 32 && d <= 128 ? 8 : 4; }
 inline int softmax_waves(int tokens, int batch, int sequences, int heads, int most, int terms) {
   auto rounds = [&](int waves) {

@@ -9,10 +9,13 @@ most.  So, with A = sum of p |v| and n keys:
 Backward, p = exp(score - lse) is off by b = 2 a + u + 2 e |lse| + (n + 8) e relative, t = do . v - D by the error of o in D and by
 (d + 2) e of the terms' magnitudes, ds = p t by p (b |t| + its error), and both are rounded, by u; sums over n more terms add (n + 8) e.
 fp16 numbers below 2^-14 are rounded to a step of 2^-24, which p (forward: times 1 or less, backward: times 2^12) and ds (times 2^15
-over twice the largest |do| |v| at the least a quarter of that) may be."""
+over twice the largest |do| |v| at the least a quarter of that) may be.
+An exponential under 2^-126 is 0, and so is an operand of a product in bf16 or fp32: p is off by 2^-126 for either, o relative to its row's
+weights by no more, ds = p t by |t| times that and by 2^-126 for itself as an operand."""
 import torch
 
 E = 2.0 ** -24
+ZERO = 2 * 2.0 ** -126
 
 
 def unit(dtype):
@@ -69,7 +72,7 @@ def attention(q, k, v, causal, where, scale=None, do=None):
             n = seen.sum(-1, keepdim=True).double()
             a = (d + 2) * E * size + 4 * E * (2 * size + 6)
             A, o = p @ z.abs(), p @ z
-            do_o = (2 * a + 2 * u + (n + 8) * E) * A + fine * (seen.double() @ z.abs())
+            do_o = (2 * a + 2 * u + (n + 8) * E) * A + (fine + ZERO) * (seen.double() @ z.abs())
             res["out"][0][b, h, rows] = o
             res["out"][1][b, h, rows] = round_out * (o.abs() + do_o) + do_o + smallest(dtype)
             level = lse.masked_fill(empty, 0.0)
@@ -86,8 +89,9 @@ def attention(q, k, v, causal, where, scale=None, do=None):
             dt = (d + 2) * E * (g.abs() @ z.abs().t() + (g * o).abs().sum(-1, keepdim=True)) + \
                 (g.abs() * off_o).sum(-1, keepdim=True)
             ds = p * t
-            off_p = p * (rel + u) + (fine * 2.0 ** -12 * seen)
+            off_p = p * (rel + u) + (fine * 2.0 ** -12 + ZERO) * seen
             off_s = p * (rel * t.abs() + dt) * (1 + u) + u * ds.abs() + (fine * peak * 2.0 ** -12 * seen) + 4 * E * p * (t.abs() + D.abs())
+            off_s = off_s + ZERO * (t.abs() + 1) * seen
             sums = (max(nq * group, nk) + 8) * E
             res["dQ"][0][b, h, rows] = c * (ds @ y)
             res["dQ"][1][b, h, rows] = c * (off_s @ y.abs() + sums * (ds.abs() @ y.abs()))

@@ -1,0 +1,249 @@
+"""Softmax attention where it can go wrong: what lies in rows of no sequence, lengths that leave the tensors, far and repeated rows, other
+streams, captured graphs, scores that rise along the keys, gradients at the ends of fp16's range, a great many blocks."""
+import pytest
+import torch
+
+from tests import softmax_reference as ref
+from tests.test_gpu_softmax import DT, close, ints, mixed, tokens
+
+pytestmark = pytest.mark.gpu
+
+
+def run(q, k, v, g, out=None, grads=None, **kw):
+    from paper_2312_08874_amd import binding
+    o, saved = binding.agent_softmax_attn_fwd(q, k, v, save=True, out=out, **kw)
+    return o, binding.agent_softmax_attn_bwd(q, k, v, o, saved, g, grads=grads, **kw)
+
+
+def inputs(dtype, B, Hq, Hk, nq, nk, d, layout="token", seed=11, std=1.0):
+    gen = torch.Generator().manual_seed(seed)
+    q, g = (tokens(gen, DT[dtype], B, Hq, nq, d, layout, std) for _ in range(2))
+    k, v = (tokens(gen, DT[dtype], B, Hk, nk, d, layout, std) for _ in range(2))
+    return q, k, v, g
+
+
+def check(q, k, v, g, causal, where, scale=None, **kw):
+    want = ref.attention(q, k, v, causal, where, scale, do=g)
+    if scale:
+        kw["scale"] = scale
+    out, grads = run(q, k, v, g, causal=causal, **kw)
+    close(out, want["out"], "out")
+    for n in grads:
+        close(grads[n], want[n], n)
+
+
+# dtype, heads, queries, keys, d, mix
+UNUSED = [
+    ("bf16", (2, 1), 100, 170, 64, ("padded", [100, 33, 0], [170, 40, 64])),
+    ("f16", (4, 2), 1, 1800, 128, ("padded", None, [1700, 3, 0])),
+    ("f32", (2, 2), 90, 90, 48, ("padded", [64, 1, 89], [64, 1, 89])),
+    ("f16", (2, 2), 40, 70, 33, ("padded", [40, 17, 0], [70, 5, 64])),
+    ("bf16", (4, 1), 160, 260, 64, ("packed", [60, 0, 41, 1, 30], [64, 7, 90, 0, 33])),
+    ("f32", (2, 1), 100, 90, 30, ("packed", [31, 33, 10], [32, 1, 33])),
+    ("f16", (1, 1), 8, 5000, 80, ("packed", [1, 1, 1, 2], [1000, 33, 0, 2900])),
+    ("f32", (2, 2), 3, 1300, 200, ("padded", [3, 0, 2], [1300, 1, 700])),
+]
+
+
+@pytest.mark.parametrize("causal", [False, True], ids=["all", "causal"])
+@pytest.mark.parametrize("case", UNUSED, ids=[str(i) for i in range(len(UNUSED))])
+def test_rows_of_no_sequence_are_neither_read_nor_written(case, causal):
+    dtype, (hq, hk), nq, nk, d, mix = case
+    B = 1 if mix[0] == "packed" else 3
+    q, k, v, g = inputs(dtype, B, hq, hk, nq, nk, d)
+    kw, where = mixed(mix, B, nq, nk)
+    clean = run(q, k, v, g, causal=causal, **kw)
+    used_q, used_k = torch.zeros(B, nq, dtype=torch.bool), torch.zeros(B, nk, dtype=torch.bool)
+    for b, q0, n, k0, m in where:
+        used_q[b, q0:q0 + n], used_k[b, k0:k0 + m] = True, True
+    junk = torch.tensor([float("nan"), float("inf"), -float("inf"), torch.finfo(DT[dtype]).max, torch.finfo(DT[dtype]).min]).to(DT[dtype]).cuda()
+    dirty = []
+    for t, used in ((q, used_q), (k, used_k), (v, used_k), (g, used_q)):
+        t = t.clone()
+        rows = ~used[:, None, :, None].expand(t.shape).cuda()
+        t[rows] = junk[torch.arange(int(rows.sum()), device="cuda") % 5]
+        dirty.append(t)
+    marks = [torch.full_like(t, 7.0) for t in (q, q, k, v)]
+    out, grads = run(*dirty, out=marks[0], grads=marks[1:], causal=causal, **kw)
+    for got, want, used in ((out, clean[0], used_q), (grads["dQ"], clean[1]["dQ"], used_q), (grads["dK"], clean[1]["dK"], used_k),
+                            (grads["dV"], clean[1]["dV"], used_k)):
+        rows = used[:, None, :, None].expand(got.shape).cuda()
+        assert torch.equal(got[rows], want[rows])
+        assert bool((got[~rows] == 7.0).all()) and bool((want[~rows] == 0.0).all())
+
+
+def test_lengths_and_starts_are_kept_within_the_tensors():
+    from paper_2312_08874_amd import binding
+    q, k, v, g = inputs("bf16", 4, 2, 1, 50, 70, 64)
+    wild = run(q, k, v, g, lengths=(ints([-3, 60, 2 ** 31 - 1, 7]), ints([99, -2 ** 31, 70, 2 ** 30])))
+    tame = run(q, k, v, g, lengths=(ints([0, 50, 50, 7]), ints([70, 0, 70, 70])))
+    assert torch.equal(wild[0], tame[0]) and all(torch.equal(wild[1][n], tame[1][n]) for n in tame[1])
+    # starts that rise beyond the rows end there; any others leave what is around the tensors alone
+    q, k, v, g = inputs("f16", 1, 2, 1, 150, 200, 64)
+    wild = run(q, k, v, g, starts=(ints([-5, 100, 170, 400]), ints([0, 90, 200, 2 ** 31 - 1])))
+    tame = run(q, k, v, g, starts=(ints([0, 100, 150, 150]), ints([0, 90, 200, 200])))
+    assert torch.equal(wild[0], tame[0]) and all(torch.equal(wild[1][n], tame[1][n]) for n in tame[1])
+    for sq, sk in (([140, 3, 90, -7, 150], [0, 200, 10, 190, 3]), ([2 ** 31 - 1, -2 ** 31, 2 ** 30, 0, 64], [64, 64, 0, 2 ** 31 - 1, 1])):
+        room = [torch.full((1, 2 if i < 2 else 1, n + 200, 64), 3.0, dtype=torch.float16, device="cuda") for i, n in enumerate((150, 150, 200, 200))]
+        views = [r[:, :, 100:-100] for r in room]
+        starts = (ints(sq), ints(sk))
+        o, saved = binding.agent_softmax_attn_fwd(q, k, v, save=True, out=views[0], starts=starts)
+        binding.agent_softmax_attn_bwd(q, k, v, o, saved, g, grads=views[1:], starts=starts)
+        for r in room:
+            assert bool((r[:, :, :100] == 3.0).all()) and bool((r[:, :, -100:] == 3.0).all())
+
+
+@pytest.mark.parametrize("queries,step", [(1, 1 << 22), (40, 1 << 22), (130, 1 << 22), (130, (1 << 23) + 8)],
+                         ids=["one", "few", "many", "beyond_a_tile"])
+def test_rows_further_apart_than_32_bits_reach(queries, step):
+    """Keys and values of 8 MiB and more from row to row, over 4 GiB in all."""
+    heads = 1 if queries < 100 else 300
+    q, k, v, g = inputs("bf16", 1, 2 * heads, heads, queries, 600, 32, "dense")
+    near = run(q, k, v, g)
+
+    def far(t):
+        room = torch.empty(step * 600, dtype=t.dtype, device="cuda")
+        view = room.as_strided(t.shape, (0, 32, step, 1))
+        view.copy_(t)
+        return view
+    fk, fv, dk = far(k), far(v), far(torch.zeros_like(k))
+    out, grads = run(q, fk, fv, g, grads=(torch.empty_like(q), dk, torch.empty_like(v)))
+    assert torch.equal(out, near[0])
+    assert all(torch.equal(grads[n], near[1][n]) for n in grads)
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+def test_repeated_inputs(dtype):
+    q, k, v, g = inputs(dtype, 3, 4, 2, 70, 90, 64)
+    one_k, one_v, one_g = k[:1, :1].expand(k.shape), v[:, :1].expand(v.shape), g[:1].expand(g.shape)
+    got = run(q, one_k, one_v, one_g, causal=True)
+    want = run(q, one_k.contiguous(), one_v.contiguous(), one_g.contiguous(), causal=True)
+    assert torch.equal(got[0], want[0]) and all(torch.equal(got[1][n], want[1][n]) for n in want[1])
+    same = run(k, k, k, k, causal=True)                 # one tensor for all
+    apart = run(k, k.clone(), k.clone(), k.clone(), causal=True)
+    assert torch.equal(same[0], apart[0]) and all(torch.equal(same[1][n], apart[1][n]) for n in apart[1])
+
+
+@pytest.mark.parametrize("shape", [(2, 4, 2, 200, 200, 64), (4, 8, 2, 1, 3000, 64)], ids=["many", "one"])
+def test_on_another_stream(shape):
+    B, hq, hk, nq, nk, d = shape
+    q, k, v, g = inputs("f16", B, hq, hk, nq, nk, d)
+    want = run(q, k, v, g, causal=True)
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    a = run(q, k, v, g, causal=True, stream=side)      # two at once
+    b = run(q, k, v, g, causal=True)
+    with torch.cuda.stream(side):
+        c = run(q, k, v, g, causal=True)
+    torch.cuda.synchronize()
+    for got in (a, b, c):
+        assert torch.equal(got[0], want[0]) and all(torch.equal(got[1][n], want[1][n]) for n in want[1])
+
+
+@pytest.mark.parametrize("dtype,shape", [("f16", (3, 4, 2, 130, 130, 64)), ("bf16", (3, 4, 1, 1, 4000, 128)), ("f32", (3, 2, 2, 70, 90, 40))],
+                         ids=["self", "one", "terms"])
+def test_captured_and_replayed(dtype, shape):
+    """Two graphs of one call each, replayed in turn over changing inputs and lengths, with eager calls between."""
+    B, hq, hk, nq, nk, d = shape
+    graphs = []
+    for seed in (1, 2):
+        t = inputs(dtype, B, hq, hk, nq, nk, d, seed=seed)
+        lengths = (ints([nq] * B), ints([nk] * B))
+        run(*t, causal=True, lengths=lengths)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            result = run(*t, causal=True, lengths=lengths)
+        graphs.append((graph, t, lengths, result))
+    gen = torch.Generator().manual_seed(9)
+    for turn in range(4):
+        for graph, t, lengths, result in graphs:
+            for x in t:
+                x.copy_((0.5 + turn) * torch.randn(x.shape, generator=gen).to(x.dtype))
+            lengths[0].copy_(torch.randint(0, nq + 1, (B,), generator=gen))
+            lengths[1].copy_(torch.randint(0, nk + 1, (B,), generator=gen))
+        for graph, *_ in graphs:
+            graph.replay()
+        for graph, t, lengths, result in graphs:
+            want = run(*t, causal=True, lengths=lengths)
+            assert torch.equal(result[0], want[0]), turn
+            assert all(torch.equal(result[1][n], want[1][n]) for n in want[1]), turn
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+@pytest.mark.parametrize("nq,nk", [(140, 300), (2, 2600)], ids=["many", "few"])
+def test_scores_that_rise_and_fall_along_the_keys(dtype, nq, nk):
+    """Scores from -60 to 60: every tile passes what the weights are taken against, or falls far below it."""
+    B = 16 if nq > 2 else 1
+    q, k, v, g = inputs(dtype, B, 16, 16, nq, nk, 32, "dense")
+    q[..., 0], k[..., 0] = 4.0, torch.linspace(-85.0, 85.0, nk, device="cuda").to(k.dtype)
+    k[:, 1::2] = k[:, 1::2].flip(2)                   # rise, and fall
+    q, k, v, g = (t[:1, :2].contiguous() if nq == 2 else t for t in (q, k, v, g))
+    if nq > 2:      # the kernel of many queries takes them all; the oracle two
+        from paper_2312_08874_amd import binding
+        out = binding.agent_softmax_attn_fwd(q, k, v)
+        want = ref.attention(q[:1, :2], k[:1, :2], v[:1, :2], False, ref.spans(1, nq, nk))
+        close(out[:1, :2], want["out"], "out")
+        return
+    check(q, k, v, g, False, ref.spans(1, nq, nk))
+
+
+@pytest.mark.parametrize("size", [2.0 ** -22, 2.0 ** 11], ids=["small", "large"])
+def test_gradients_at_the_ends_of_fp16(size):
+    q, k, v, g = inputs("f16", 2, 2, 1, 100, 130, 64)
+    check(q, k, v, (g.float() * size).half(), True, ref.spans(2, 100, 130))
+    check(q, k, v, torch.zeros_like(g), False, ref.spans(2, 100, 130))
+
+
+@pytest.mark.parametrize("dtype", ["bf16", "f16", "f32"])
+def test_scale(dtype):
+    q, k, v, g = inputs(dtype, 2, 2, 2, 60, 80, 40)
+    check(q, k, v, g, True, ref.spans(2, 60, 80), scale=0.6)
+    check(q, k, v, g, False, ref.spans(2, 60, 80), scale=1e-30)      # weights all alike
+
+
+@pytest.mark.parametrize("nq,nk", [(200, 200), (3, 2500)], ids=["many", "few"])
+def test_a_row_that_is_nan_stays_alone(nq, nk):
+    from paper_2312_08874_amd import binding
+    q, k, v, g = inputs("bf16", 1, 2, 2, nq, nk, 64)
+    q[0, 0, nq // 2, 5] = float("nan")
+    k[0, 1, 7, 1] = float("nan")
+    out = binding.agent_softmax_attn_fwd(q, k, v)
+    assert bool(torch.isnan(out[0, 0, nq // 2]).all()) and bool(torch.isnan(out[0, 1]).all())
+    rest = torch.arange(nq) != nq // 2
+    q[0, 0, nq // 2, 5], k[0, 1, 7, 1] = 0.0, 0.0
+    want = ref.attention(q, k, v, False, ref.spans(1, nq, nk))["out"]
+    close(out[:, :1, rest], tuple(t[:, :1, rest] for t in want), "the other rows")
+
+
+@pytest.mark.parametrize("B,heads,n", [(200000, 8, 2), (140000, 8, 17)], ids=["few", "many"])
+def test_more_blocks_than_a_grid_is_wide(B, heads, n):
+    gen = torch.Generator(device="cuda").manual_seed(1)
+    q, k, v, g = (torch.randn(B, heads, n, 8, generator=gen, device="cuda").bfloat16() for _ in range(4))
+    out, grads = run(q, k, v, g, causal=True)
+    for at in (0, 131072 - 2, B - 4):
+        part = [t[at:at + 4] for t in (q, k, v, g)]
+        want = ref.attention(*part[:3], True, ref.spans(4, n, n), do=part[3])
+        close(out[at:at + 4], want["out"], "out")
+        for name in grads:
+            close(grads[name][at:at + 4], want[name], name)
+
+
+def test_prepared_calls_and_refusals():
+    from paper_2312_08874_amd import binding
+    q, k, v, g = inputs("bf16", 2, 4, 2, 30, 50, 64)
+    lengths = (None, ints([50, 50]))
+    out = torch.zeros_like(q)
+    call = binding.prepare_softmax_attn(q, k, v, causal=True, lengths=lengths, out=out)
+    for n in (50, 31, 0):
+        lengths[1].fill_(n)
+        call()
+        assert torch.equal(out, binding.agent_softmax_attn_fwd(q, k, v, causal=True, lengths=lengths)), n
+    for bad in (dict(lengths=(None, lengths[1].long())), dict(lengths=(None, lengths[1][:1])), dict(lengths=(None, lengths[1].cpu())),
+                dict(starts=(ints([0, 30]), ints([0, 50]))), dict(out=out[:, :2]), dict(out=out.float())):
+        with pytest.raises((AssertionError, RuntimeError)):
+            binding.agent_softmax_attn_fwd(q, k, v, **bad)
+    for bad in ((q, k[..., :32], v), (q, k, v[:, :1]), (q, k.float(), v), (q.cpu(), k, v), (q[:, :3], k, v), (q[:1], k, v)):
+        with pytest.raises((AssertionError, RuntimeError)):
+            binding.agent_softmax_attn_fwd(*bad)
+    with pytest.raises(RuntimeError, match="AA_ERR_ALIAS"):
+        binding.agent_softmax_attn_fwd(q, k, v, out=q)
