@@ -14,6 +14,7 @@ constexpr int kSoftmaxWidth = 256;      // most channels of a head
 // What rounding took from out is kept for queries that see up to so many keys: without it the error of D shows in dq and dk of 16-bit
 // types, which are off by 1.4 roundings with it, and by 2.2 for 2 keys, 1.6 for 64, 1.45 for 512 without.
 constexpr int kLowKeys = 512;
+constexpr int kPeakBlocks = 512;      // most blocks that look for fp16's peaks
 
 struct SoftmaxArgs {
   TokenView q, k, v, out, dout, dq, dk, dv;
@@ -28,6 +29,7 @@ struct SoftmaxArgs {
   int batch, heads_q, heads_k, tokens_q, tokens_k, d, sequences;      // sequences 0: not packed
   int causal;
   int waves;            // of a block: 2, 4 or 8, each of which has 32 rows
+  int two;              // backward: softmax_two_roundings
   int wide;             // whole 16-byte pieces wherever a result is stored
   float scale, c;       // c = scale log2 e
   // columns kernel: query heads side by side in a tile, tokens of a tile, ranges of keys and where each leaves its part
@@ -35,7 +37,8 @@ struct SoftmaxArgs {
   float *part, *part_ml;      // [split][batch, head, token][d], [..][2]
   // backward pass: what the queries' kernel leaves for the keys' of every query, [2][batch][heads_q][tokens_q], and fp16's peaks
   float* stats;
-  unsigned* peaks;      // bits of the largest squared length of a row of dout, and of v
+  float* peaks;         // [2][kPeakBlocks]: of each of peak_blocks blocks, the largest squared length of a row of dout, and of v
+  int peak_blocks;      // a multiple of eight
   // parts of dq, or of dk and dv: [split][batch, head, token][d]
   float *part_a, *part_b;
   int first_batch;      // of a launch that sums them
@@ -115,9 +118,23 @@ inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a, int es) {
   if (p.columns) {
     const long long blocks = p.tiles * outer * a.heads_q / p.pack;
     // two blocks a compute unit: 8 sequences of up to 65536 keys, 4 heads of 128 in fp16, 133 us; with one 130, with four 145, eight 166
-    p.splits = softmax_splits(blocks, 2 * kSoftmaxUnits, keys, 512);
+    // and ranges of 512 keys at the least; for single tokens of 256 up to some thousand keys and in fp32, whose tiles take long: four tokens over
+    // 2000 keys of 8 heads of 64, 12.7 us and 14.1 with 512, fp32 19.3 and 24.9, but one token over 20000 keys of 2 heads of 128 19.5 and 17.3,
+    // 64 tokens over 2 x 4096 of 8 heads 28.8 and 21.4
+    const int least = queries <= 16 && (es == 4 || keys <= 8192) ? 256 : 512;
+    p.splits = softmax_splits(blocks, 2 * kSoftmaxUnits, keys, least);
   }
   return p;
+}
+// Whether the backward pass of 16-bit types takes P and dS as two roundings, the value's and what that left: of one, gradients are off by
+// 1.41 roundings of their own, and by up to 1.56 where a head is so narrow that sums over the keys come out much smaller than their
+// terms; where they are few values, by chance more.  Up to 32 channels two cost nothing (2048 tokens, 4 x 8 heads of 16: 140 us, 140 with
+// one); in small calls of others some 3 us (256 tokens, 4 x 8 heads of 128: 46.3, 41.9 with one), of 8192 packed tokens of 8 heads of 64
+// 114 instead of 99.
+constexpr int kTwoWidth = 32;
+inline bool softmax_two_roundings(const SoftmaxArgs& a, int es) {
+  const double scores = (double)a.batch * a.heads_q * a.tokens_q * (double)softmax_typical(a.tokens_k, a.sequences);
+  return es == 2 && (a.d <= kTwoWidth || scores * a.d <= 1e8);
 }
 // The backward pass: ranges of keys for the queries' kernel, of queries (all heads that share the keys) for the keys'.
 struct SoftmaxBackPlan {
@@ -128,13 +145,16 @@ inline SoftmaxBackPlan softmax_back_plan(const SoftmaxArgs& a, int es, bool keys
   const int tokens = keys ? a.tokens_k : a.tokens_q, heads = keys ? a.heads_k : a.heads_q;
   SoftmaxBackPlan p;
   p.waves = softmax_waves(tokens, a.batch, a.sequences, heads, keys ? 4 : softmax_most_waves(es, a.d), softmax_terms(es, softmax_width(a.d)));
+  if (a.d > kTwoWidth && softmax_two_roundings(a, es)) p.waves = 2;      // so that not every kernel is there twice
   p.tiles = softmax_tiles(tokens, 1, a.sequences, 32 * p.waves);
   const long long across = keys ? softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k) : softmax_typical(a.tokens_k, a.sequences);
   // Blocks for each compute unit that ranges are to make up for.  Uneven ones (causal) are shared out better where there are more, which
   // costs their parts' way through memory: the keys' kernel of 2 x 4096 tokens, 16 heads on 4 of 128, and its sum take 383 us with two
   // ranges, 315 with three, 328 with four; of 2 x 2000 tokens, 8 heads of 80, a step takes 229 with two and 247 with three.
   const int each = keys ? (a.causal && across >= 8192 ? 3 : 2) : a.causal ? 2 : 1;
-  p.splits = softmax_splits(p.tiles * (a.sequences > 0 ? 1 : a.batch) * heads, each * kSoftmaxUnits, across, 512);
+  // and each range of 512 at the least, in fp32, whose tiles take long, 128: 1000 tokens, 6 heads of 48, 159 us with 512, 113 with 256, 102 so;
+  // 2048 tokens, 8 heads of 64 in bf16 104 with 512, 128 with 256 and twice the blocks
+  p.splits = softmax_splits(p.tiles * (a.sequences > 0 ? 1 : a.batch) * heads, each * kSoftmaxUnits, across, es == 4 ? 128 : 512);
   return p;
 }
 

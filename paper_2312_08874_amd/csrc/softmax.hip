@@ -8,6 +8,7 @@ namespace {
 
 constexpr size_t kAlign = 256;
 size_t aligned(size_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
+constexpr size_t kPeakBytes = 2 * kPeakBlocks * sizeof(float);
 
 struct Tensor {
   TokenView* view;
@@ -187,14 +188,18 @@ size_t softmax_bwd_workspace(int dtype, const SoftmaxArgs& a) {
   // the queries' parts are added up before the keys' are written
   const size_t parts = std::max(sq > 1 ? aligned((size_t)sq * query_rows(a) * a.d * 4) : 0,
                                 sk > 1 ? 2 * aligned((size_t)sk * key_rows(a) * a.d * 4) : 0);
-  return kAlign + aligned((size_t)query_rows(a) * 8) + q + k + v + g + parts;
+  return (dtype == 1 ? kPeakBytes : 0) + aligned((size_t)query_rows(a) * 8) + q + k + v + g + parts;
 }
 
 hipError_t launch_softmax_bwd(int dtype, SoftmaxArgs a, void* workspace, hipStream_t st) {
   const int es = dtype == 0 ? 4 : 2, terms = softmax_terms(es, softmax_width(a.d));
   char* ws = (char*)workspace;
   a.dout_whole = a.dout;
-  a.peaks = (unsigned*)ws, ws += kAlign;
+  if (dtype == 1) {
+    const long long blocks = (std::max(query_rows(a), key_rows(a)) + 127) / 128;
+    a.peaks = (float*)ws, ws += kPeakBytes;
+    a.peak_blocks = (int)std::min<long long>((blocks + 7) / 8 * 8, kPeakBlocks);
+  }
   a.stats = (float*)ws, ws += aligned((size_t)query_rows(a) * 8);
   a.wide = 1;
   for (const TokenView* v : {&a.out, &a.dq, &a.dout_whole}) a.wide = a.wide && wide_result(*v, a.batch, a.heads_q, a.tokens_q, a.d, es);
@@ -203,6 +208,7 @@ hipError_t launch_softmax_bwd(int dtype, SoftmaxArgs a, void* workspace, hipStre
   if (err == hipSuccess && dtype == 1) err = launch(dtype, a, SoftmaxPass::kPeaks, 0, st);
   if (err != hipSuccess) return err;
   const SoftmaxBackPlan q = softmax_back_plan(a, es, false), k = softmax_back_plan(a, es, true);
+  a.two = softmax_two_roundings(a, es);
   a.waves = q.waves, a.splits = q.splits;
   a.part_a = (float*)ws;
   err = launch(dtype, a, SoftmaxPass::kQueries, q.tiles, st);

@@ -108,7 +108,9 @@ def test_workspaces():
     assert parts > 0 and parts % 256 == 0
     assert fwd(long) == -5
     assert need(desc(d=300)) == 0 and need(desc(d=300), back=True) == 0
-    assert need(desc(), back=True) >= 256 + 2 * 4 * 2 * 4 * 12
+    rows = 2 * 4 * 12
+    assert need(desc(), back=True) == 8 * rows                         # two statistics a query
+    assert need(desc(dtype=binding.AA_F16), back=True) == 4096 + 8 * rows      # and the blocks' largest rows of dout and v
     L = binding.lib()
     assert L.agent_softmax_attn_saved_bytes(ctypes.byref(desc())) == 512 + 2 * 4 * 12 * 32 * 2
     assert L.agent_softmax_attn_saved_bytes(ctypes.byref(desc(dtype=binding.AA_F32))) == 512
@@ -161,6 +163,7 @@ def test_which_kernel_takes_what(rules):
         p = rules(*case)
         assert p["tiles"] == case[3] // p["tile_tokens"] + case[7]
         assert p["dkv_tiles"] == case[4] // (32 * p["dkv_waves"]) + case[7]
+    assert rules(1, 2, 2, 200, 200, 128)["dkv_waves"] == 2 == rules(1, 2, 2, 200, 200, 128)["dq_waves"]      # two roundings: two waves
     for hq, hk in ((1, 1), (6, 2), (5, 1), (12, 3), (64, 1), (7, 7)):
         p = rules(3, hq, hk, 1, 5000, 64)
         assert (hq // hk) % p["pack"] == 0 and 1 <= p["pack"] <= 32 and p["tile_tokens"] == 32 // p["pack"]
