@@ -1122,8 +1122,12 @@ def agent_layer_norm_fwd(x, weight=None, bias=None, *, residual=None, eps=1e-5, 
         sum_out = _dense_like(x, stream)
     saved = None
     if save:
-        with torch.cuda.stream(stream):      # None: the current one
-            saved = torch.empty((x.numel() // x.shape[-1], 2), dtype=torch.float32, device=x.device)
+        shape = (x.numel() // x.shape[-1], 2)
+        if stream is None:      # entering a stream costs the host as much as a launch
+            saved = torch.empty(shape, dtype=torch.float32, device=x.device)
+        else:
+            with torch.cuda.stream(stream):
+                saved = torch.empty(shape, dtype=torch.float32, device=x.device)
     _check(lib().agent_layer_norm_fwd(*_layer_norm_args(x, weight, bias, residual, eps, saved, out, sum_out, stream)), "agent_layer_norm_fwd")
     results = (out,) + (() if sum_out is None else (sum_out,)) + ((saved,) if save else ())
     return results if len(results) > 1 else out
