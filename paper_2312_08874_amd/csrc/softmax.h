@@ -29,6 +29,7 @@ struct SoftmaxArgs {
   int batch, heads_q, heads_k, tokens_q, tokens_k, d, sequences;      // sequences 0: not packed
   int causal;
   int waves;            // of a block: 2, 4 or 8, each of which has 32 rows
+  int shared;           // softmax_shared
   int two;              // backward: softmax_two_roundings
   int wide;             // whole 16-byte pieces wherever a result is stored
   float scale, c;       // c = scale log2 e
@@ -69,23 +70,32 @@ constexpr int softmax_column_waves(int es, int dp) { return es * dp <= 256 ? 4 :
 
 constexpr int kSoftmaxUnits = 256;      // compute units
 
+// Whether blocks are of 64 rows and two waves share every 32 of them, each with half of every tile of 64 keys (or queries): where there are so
+// few blocks that the length of the longest is the time, and not so long ones that ranges are worth their parts.  `blocks`: of 64 rows,
+// `across`: what each goes over.  Measured, training steps, shared and not: 1500 tokens, 2 x 8
+// heads of 64, causal, 63 us and 88; 2 x 2000, 8 heads of 80 120 and 140; 4096, 8 heads of 64 187 and 214; but 8192 packed tokens, 8 heads, 1184
+// blocks, 108 and 100, and 2 x 1900, 16 heads of 128, 960 blocks, 427 and 355;
+// 2 x 4096, 16 heads on 4 of 128, whose keys are seen by 16384 rows, 919 and 648.
+inline bool softmax_shared(int es, long long blocks, long long across) { return es == 2 && blocks < 3 * kSoftmaxUnits && across < 8192; }
+
 // Waves of a block of rows, 32 rows each: as few rounds of blocks over the compute units as may be, two waves where four would be half
 // empty, eight, which share every tile of keys, where they cost no round.  Measured: windows of 49 tokens, 2048 x 12 heads, 79 us with two
 // and 96 with four; 37 packed images of 8192 tokens in all, a training step, 101 and 110; 128 x 128 tokens, 2359 with eight (forward and
 // for dq), 2432 with four, 2912 with two.  Terms take three times the LDS: two waves then cost more.
 constexpr int softmax_most_waves(int es, int d) { return es == 2 && d > 32 && d <= 128 ? 8 : 4; }
-inline int softmax_waves(int tokens, int batch, int sequences, int heads, int most, int terms) {
+inline int softmax_waves(int es, int tokens, int batch, int sequences, int heads, long long across, int most, int terms) {
   auto rounds = [&](int waves) {
     const long long blocks = softmax_tiles(tokens, batch, sequences, 32 * waves) * heads;
     return (blocks + kSoftmaxUnits - 1) / kSoftmaxUnits * waves;
   };
+  if (softmax_shared(es, softmax_tiles(tokens, batch, sequences, 64) * heads, across)) return 2;
   const int waves = rounds(2) * (terms > 1 ? 3 : 2) < rounds(4) * 2 ? 2 : 4;
   return most >= 8 && rounds(8) <= rounds(waves) ? 8 : waves;
 }
 
 struct SoftmaxPlan {
   int waves;
-  bool columns;
+  bool columns, shared;
   int pack, tile_tokens, splits;
   long long tiles;      // of queries
 };
@@ -102,7 +112,7 @@ inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a, int es) {
   SoftmaxPlan p{};
   const int group = a.heads_q / a.heads_k, outer = a.sequences > 0 ? 1 : a.batch;
   const long long queries = softmax_typical(a.tokens_q, a.sequences), keys = softmax_typical(a.tokens_k, a.sequences);
-  p.waves = softmax_waves(a.tokens_q, a.batch, a.sequences, a.heads_q, softmax_most_waves(es, a.d), softmax_terms(es, softmax_width(a.d)));
+  p.waves = softmax_waves(es, a.tokens_q, a.batch, a.sequences, a.heads_q, keys, softmax_most_waves(es, a.d), softmax_terms(es, softmax_width(a.d)));
   const long long row_blocks = softmax_tiles(a.tokens_q, a.batch, a.sequences, 128) * a.heads_q;
   p.columns = queries <= 16 || (row_blocks < kSoftmaxUnits && keys >= (es == 4 ? 512 : 1536));
   p.pack = 1, p.tile_tokens = 32 * p.waves, p.splits = 1;
@@ -113,6 +123,7 @@ inline SoftmaxPlan softmax_plan(const SoftmaxArgs& a, int es) {
         if (group % n == 0 && (queries * n <= 32 || n <= 4)) p.pack = n;
     p.tile_tokens = 32 / p.pack;
   }
+  p.shared = !p.columns && p.waves == 2 && softmax_shared(es, softmax_tiles(a.tokens_q, a.batch, a.sequences, 64) * a.heads_q, keys);
   p.tiles = softmax_tiles(a.tokens_q, outer, a.sequences, p.tile_tokens);
   if (a.sequences == 0) p.tiles /= outer;
   if (p.columns) {
@@ -139,22 +150,25 @@ inline bool softmax_two_roundings(const SoftmaxArgs& a, int es) {
 // The backward pass: ranges of keys for the queries' kernel, of queries (all heads that share the keys) for the keys'.
 struct SoftmaxBackPlan {
   int waves, splits;
+  bool shared;
   long long tiles;      // of one sequence, or of the packed run
 };
 inline SoftmaxBackPlan softmax_back_plan(const SoftmaxArgs& a, int es, bool keys) {
   const int tokens = keys ? a.tokens_k : a.tokens_q, heads = keys ? a.heads_k : a.heads_q;
   SoftmaxBackPlan p;
-  p.waves = softmax_waves(tokens, a.batch, a.sequences, heads, keys ? 4 : softmax_most_waves(es, a.d), softmax_terms(es, softmax_width(a.d)));
+  const long long across = keys ? softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k) : softmax_typical(a.tokens_k, a.sequences);
+  p.waves = softmax_waves(es, tokens, a.batch, a.sequences, heads, across, keys ? 4 : softmax_most_waves(es, a.d), softmax_terms(es, softmax_width(a.d)));
   if (a.d > kTwoWidth && softmax_two_roundings(a, es)) p.waves = 2;      // so that not every kernel is there twice
   p.tiles = softmax_tiles(tokens, 1, a.sequences, 32 * p.waves);
-  const long long across = keys ? softmax_typical(a.tokens_q, a.sequences) * (a.heads_q / a.heads_k) : softmax_typical(a.tokens_k, a.sequences);
   // Blocks for each compute unit that ranges are to make up for.  Uneven ones (causal) are shared out better where there are more, which
   // costs their parts' way through memory: the keys' kernel of 2 x 4096 tokens, 16 heads on 4 of 128, and its sum take 383 us with two
   // ranges, 315 with three, 328 with four; of 2 x 2000 tokens, 8 heads of 80, a step takes 229 with two and 247 with three.
   const int each = keys ? (a.causal && across >= 8192 ? 3 : 2) : a.causal ? 2 : 1;
   // and each range of 512 at the least, in fp32, whose tiles take long, 128: 1000 tokens, 6 heads of 48, 159 us with 512, 113 with 256, 102 so;
   // 2048 tokens, 8 heads of 64 in bf16 104 with 512, 128 with 256 and twice the blocks
-  p.splits = softmax_splits(p.tiles * (a.sequences > 0 ? 1 : a.batch) * heads, each * kSoftmaxUnits, across, es == 4 ? 128 : 512);
+  const long long blocks = p.tiles * (a.sequences > 0 ? 1 : a.batch) * heads;
+  p.shared = p.waves == 2 && softmax_shared(es, blocks, across);
+  p.splits = softmax_splits(blocks, each * kSoftmaxUnits / (p.shared ? 2 : 1), across, es == 4 ? 128 : 512);
   return p;
 }
 

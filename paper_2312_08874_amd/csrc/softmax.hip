@@ -171,7 +171,7 @@ hipError_t launch_softmax_fwd(int dtype, SoftmaxArgs a, void* workspace, hipStre
   a.wide = wide_result(a.out, a.batch, a.heads_q, a.tokens_q, a.d, es);
   hipError_t err = take_inputs(a, ws, es, terms, false, st);
   if (err != hipSuccess) return err;
-  a.waves = p.waves, a.pack = p.pack, a.tile_tokens = p.tile_tokens, a.splits = p.splits;
+  a.waves = p.waves, a.shared = p.shared, a.pack = p.pack, a.tile_tokens = p.tile_tokens, a.splits = p.splits;
   if (p.splits > 1) {
     a.part = (float*)ws;
     a.part_ml = (float*)(ws + aligned((size_t)p.splits * query_rows(a) * a.d * 4));
@@ -209,12 +209,12 @@ hipError_t launch_softmax_bwd(int dtype, SoftmaxArgs a, void* workspace, hipStre
   if (err != hipSuccess) return err;
   const SoftmaxBackPlan q = softmax_back_plan(a, es, false), k = softmax_back_plan(a, es, true);
   a.two = softmax_two_roundings(a, es);
-  a.waves = q.waves, a.splits = q.splits;
+  a.waves = q.waves, a.shared = q.shared, a.splits = q.splits;
   a.part_a = (float*)ws;
   err = launch(dtype, a, SoftmaxPass::kQueries, q.tiles, st);
   if (err == hipSuccess && a.splits > 1) err = launch(dtype, a, SoftmaxPass::kSumQueries, 0, st);
   if (err != hipSuccess) return err;
-  a.waves = k.waves, a.splits = k.splits;
+  a.waves = k.waves, a.shared = k.shared, a.splits = k.splits;
   a.part_b = (float*)(ws + aligned((size_t)a.splits * key_rows(a) * a.d * 4));
   err = launch(dtype, a, SoftmaxPass::kKeys, k.tiles, st);
   return err != hipSuccess || a.splits == 1 ? err : launch(dtype, a, SoftmaxPass::kSumKeys, 0, st);

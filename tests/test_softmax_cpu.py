@@ -129,7 +129,7 @@ int main(int argc, char** argv) {
   a.batch = v[0], a.heads_q = v[1], a.heads_k = v[2], a.tokens_q = v[3], a.tokens_k = v[4], a.d = v[5], a.causal = v[6], a.sequences = v[7];
   const SoftmaxPlan p = softmax_plan(a, v[8]);
   const SoftmaxBackPlan q = softmax_back_plan(a, v[8], false), k = softmax_back_plan(a, v[8], true);
-  printf("%d %d %d %d %d %lld %d %d %lld %d %d %lld\n", p.columns, p.waves, p.pack, p.tile_tokens, p.splits, p.tiles, q.waves, q.splits, q.tiles,
+  printf("%d %d %d %d %d %d %d %d %lld %d %d %lld %d %d %lld\n", p.shared, q.shared, k.shared, p.columns, p.waves, p.pack, p.tile_tokens, p.splits, p.tiles, q.waves, q.splits, q.tiles,
          k.waves, k.splits, k.tiles);
 }
 '''
@@ -144,7 +144,7 @@ def rules(tmp_path_factory):
 
     def plan(B, Hq, Hk, nq, nk, d, causal=0, sequences=0, es=2):
         out = subprocess.run([str(exe)] + [str(x) for x in (B, Hq, Hk, nq, nk, d, causal, sequences, es)], check=True, capture_output=True, text=True)
-        names = ("columns", "waves", "pack", "tile_tokens", "splits", "tiles", "dq_waves", "dq_splits", "dq_tiles", "dkv_waves", "dkv_splits", "dkv_tiles")
+        names = ("shared", "dq_shared", "dkv_shared", "columns", "waves", "pack", "tile_tokens", "splits", "tiles", "dq_waves", "dq_splits", "dq_tiles", "dkv_waves", "dkv_splits", "dkv_tiles")
         return dict(zip(names, (int(x) for x in out.stdout.split())))
     return plan
 
@@ -158,6 +158,9 @@ def test_which_kernel_takes_what(rules):
     assert rules(2048, 12, 12, 49, 49, 32)["waves"] == 2                  # half of 128 rows would be empty
     assert rules(1, 2, 2, 64, 20000, 64)["columns"]                       # few blocks, long keys
     assert not rules(1, 2, 2, 64, 300, 64)["columns"]
+    few = rules(2, 8, 8, 1500, 1500, 64)                                  # 384 blocks of 64 rows, whose keys two waves share
+    assert few["waves"] == few["dq_waves"] == few["dkv_waves"] == 2 and few["shared"] and few["dq_shared"] and few["dkv_shared"]
+    assert not rules(2, 8, 8, 1500, 1500, 64, es=4)["shared"] and not big["shared"] and not one["shared"]
     # every token has a tile, whatever the lengths on the device are
     for case in ((1, 4, 2, 1000, 1300, 64, 0, 7), (1, 4, 4, 70, 900, 64, 1, 70), (1, 8, 1, 33, 5, 128, 0, 1), (1, 1, 1, 1, 1, 8, 0, 1)):
         p = rules(*case)
