@@ -10,18 +10,43 @@ constexpr size_t kAlign = 256;
 size_t aligned(size_t bytes) { return (bytes + kAlign - 1) / kAlign * kAlign; }
 constexpr size_t kPeakBytes = 2 * kPeakBlocks * sizeof(float);
 
-struct Tensor {
-  TokenView* view;
-  int heads, tokens;
+// Rows of d elements of ES bytes, at any address of an element, to dense rows of whole 16-byte pieces, zeros behind their end: a piece a
+// thread; along y the tensors.
+struct CopyOf {
+  TokenView from;
+  char* to;
+  int heads, tokens, units;      // units: heads of all batch elements
 };
-
-// rows of d elements to dense rows of `width`, with zeros behind them
-template <class T>
-__global__ __launch_bounds__(256) void softmax_copy_kernel(TokenView from, T* to, int heads, int tokens, int d, int width, long long count) {
-  for (long long at = 256 * ((long long)blockIdx.x) + threadIdx.x; at < count; at += 256 * (long long)gridDim.x) {
-    const int c = (int)(at % width);
-    const long long row = at / width, i = row % tokens, h = row / tokens % heads, b = row / tokens / heads;
-    to[at] = c < d ? reinterpret_cast<const T*>(from.data)[b * from.sb + h * from.sh + i * from.sn + c] : (T)0;
+struct CopyArgs {
+  CopyOf t[4];
+  int d, pieces;
+};
+template <int ES>
+__global__ __launch_bounds__(256) void softmax_copy_kernel(CopyArgs a) {
+  typedef uint32_t OffWord __attribute__((ext_vector_type(4), aligned(4)));
+  typedef uint32_t OffHalf __attribute__((ext_vector_type(4), aligned(2)));
+  using AnyPiece = std::conditional_t<ES == 4, OffWord, OffHalf>;
+  using T = std::conditional_t<ES == 4, uint32_t, uint16_t>;
+  constexpr int PER = 16 / ES;
+  const CopyOf& x = a.t[blockIdx.y];
+  const int rows = 256 / a.pieces, slot = threadIdx.x / a.pieces, piece = threadIdx.x - slot * a.pieces;
+  if (slot >= rows) return;
+  const int at = blockIdx.x * rows + slot, stride = rows * gridDim.x, skip = stride / x.tokens, rest = stride % x.tokens;
+  int unit = at / x.tokens, i = at % x.tokens;
+  while (unit < x.units) {
+    const int b = unit / x.heads, h = unit - b * x.heads;
+    const T* p = reinterpret_cast<const T*>(x.from.data) + (long long)b * x.from.sb + (long long)h * x.from.sh + (long long)i * x.from.sn + piece * PER;
+    u32x4 v = {0u, 0u, 0u, 0u};
+    if ((piece + 1) * PER <= a.d) {
+      v = __builtin_bit_cast(u32x4, *reinterpret_cast<const AnyPiece*>(p));
+    } else {
+#pragma unroll
+      for (int n = 0; n < PER - 1; ++n)
+        if (piece * PER + n < a.d) v[n * ES / 4] |= (uint32_t)p[n] << (8 * (n * ES % 4));
+    }
+    *reinterpret_cast<u32x4*>(x.to + (((long long)unit * x.tokens + i) * a.pieces + piece) * 16) = v;
+    unit += skip, i += rest;
+    if (i >= x.tokens) i -= x.tokens, ++unit;
   }
 }
 // fp32 rows to dense rows of three terms, 8 * pieces bf16 values each: eight channels a thread; along y the tensors
@@ -79,19 +104,6 @@ size_t copy_bytes(const TokenView& v, int batch, int heads, int tokens, int d, i
   return aligned((size_t)batch * heads * tokens * padded(d, es) * es);
 }
 
-hipError_t copy_to(TokenView& v, char*& ws, int batch, int heads, int tokens, int d, int es, hipStream_t st) {
-  const size_t bytes = copy_bytes(v, batch, heads, tokens, d, es, 1);
-  if (bytes == 0) return hipSuccess;
-  const int width = padded(d, es);
-  const long long count = (long long)batch * heads * tokens * width;
-  const unsigned blocks = (unsigned)std::min<long long>((count + 255) / 256, 1 << 16);
-  if (es == 4) softmax_copy_kernel<uint32_t><<<blocks, 256, 0, st>>>(v, (uint32_t*)ws, heads, tokens, d, width, count);
-  else softmax_copy_kernel<uint16_t><<<blocks, 256, 0, st>>>(v, (uint16_t*)ws, heads, tokens, d, width, count);
-  v = TokenView{ws, (long long)heads * tokens * width, (long long)tokens * width, width};
-  ws += bytes;
-  return hipGetLastError();
-}
-
 // q, k, v and, of the backward pass, dout in a form that the kernels can take, in the workspace where they lie in none
 hipError_t take_inputs(SoftmaxArgs& a, char*& ws, int es, int terms, bool back, hipStream_t st) {
   TokenView* const views[] = {&a.q, &a.k, &a.v, &a.dout};
@@ -113,12 +125,26 @@ hipError_t take_inputs(SoftmaxArgs& a, char*& ws, int es, int terms, bool back, 
     softmax_terms_kernel<<<dim3(std::min((most + 255) / 256, 1u << 13), (unsigned)count), 256, 0, st>>>(t);
     return hipGetLastError();
   }
+  CopyArgs c{};
+  c.d = a.d, c.pieces = padded(a.d, es) * es / 16;
+  int copies = 0;
+  long long most = 0;
   for (int i = 0; i < count; ++i) {
     const bool keys = i == 1 || i == 2;
-    const hipError_t err = copy_to(*views[i], ws, a.batch, keys ? a.heads_k : a.heads_q, keys ? a.tokens_k : a.tokens_q, a.d, es, st);
-    if (err != hipSuccess) return err;
+    const int heads = keys ? a.heads_k : a.heads_q, tokens = keys ? a.tokens_k : a.tokens_q, width = padded(a.d, es);
+    const size_t bytes = copy_bytes(*views[i], a.batch, heads, tokens, a.d, es, 1);
+    if (bytes == 0) continue;
+    c.t[copies++] = CopyOf{*views[i], ws, heads, tokens, a.batch * heads};
+    most = std::max(most, (long long)a.batch * heads * tokens);
+    *views[i] = TokenView{ws, (long long)heads * tokens * width, (long long)tokens * width, width};
+    ws += bytes;
   }
-  return hipSuccess;
+  if (copies == 0) return hipSuccess;
+  const long long rows = 256 / c.pieces;
+  const dim3 grid((unsigned)std::min<long long>((most + rows - 1) / rows, 1 << 12), (unsigned)copies);
+  if (es == 4) softmax_copy_kernel<4><<<grid, 256, 0, st>>>(c);
+  else softmax_copy_kernel<2><<<grid, 256, 0, st>>>(c);
+  return hipGetLastError();
 }
 
 hipError_t launch(int dtype, const SoftmaxArgs& a, SoftmaxPass pass, long long tiles, hipStream_t st) {
