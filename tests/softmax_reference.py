@@ -36,8 +36,9 @@ def spans(B, nq, nk, starts=None, lengths=None):
     return [(b, 0, q, 0, k) for b, (q, k) in enumerate(zip(lq, lk))]
 
 
-def attention(q, k, v, causal, where, scale=None, do=None):
-    """{"out", "lse"} and, with do, {"dQ", "dK", "dV"}: each (value, bound), rows of no sequence 0 (lse -inf) with bound 0."""
+def attention(q, k, v, causal, where, scale=None, do=None, peak=0.0):
+    """{"out", "lse"} and, with do, {"dQ", "dK", "dV"}: each (value, bound), rows of no sequence 0 (lse -inf) with bound 0.
+    peak: of the call's rows, where these are some of them, the largest |do| |v|."""
     dtype = q.dtype
     u = 0.0 if dtype == torch.float32 else unit(dtype)
     fine = 2.0 ** -25 if dtype == torch.float16 else 0.0
@@ -50,8 +51,7 @@ def attention(q, k, v, causal, where, scale=None, do=None):
     res = {n: [torch.zeros_like(t), torch.zeros_like(t)] for n, t in (("out", Q), ("dQ", Q), ("dK", K), ("dV", V))}
     res["lse"] = [torch.full((B, H, N), -float("inf"), dtype=torch.float64), torch.zeros(B, H, N, dtype=torch.float64)]
     res["used_q"], res["used_k"] = torch.zeros(B, N, dtype=torch.bool), torch.zeros(B, K.shape[2], dtype=torch.bool)
-    peak = 0.0
-    if G is not None:
+    if G is not None and not peak:
         peak = max((G[b, :, a:a + n].norm(dim=-1).max().item() for b, a, n, _, _ in where if n), default=0.0) * \
             max((V[b, :, a:a + n].norm(dim=-1).max().item() for b, _, _, a, n in where if n), default=0.0)
     for b, q0, nq, k0, nk in where:

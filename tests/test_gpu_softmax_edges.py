@@ -246,6 +246,26 @@ def test_more_blocks_than_a_grid_is_wide(B, heads, n):
             close(grads[name][at:at + 4], want[name], name)
 
 
+@pytest.mark.parametrize("dtype,d", [("bf16", 32), ("f16", 40), ("bf16", 64), ("f16", 80), ("bf16", 96), ("f16", 128), ("bf16", 200), ("f32", 32), ("f32", 64),
+                                     ("f32", 128), ("f32", 144)])
+@pytest.mark.parametrize("causal", [False, True], ids=["all", "causal"])
+def test_blocks_of_many_waves(dtype, d, causal):
+    """Enough blocks for four and eight waves of each: two of the batch's sequences are looked at, of which one is short."""
+    B, heads, n = 32, 8, 250
+    gen = torch.Generator(device="cuda").manual_seed(2)
+    q, k, v, g = (torch.randn(B, n, heads, d, generator=gen, device="cuda").to(DT[dtype]).permute(0, 2, 1, 3) for _ in range(4))
+    lengths = torch.randint(1, n + 1, (B,), generator=torch.Generator().manual_seed(3), dtype=torch.int32)
+    lengths[0], lengths[B - 1] = n, 131
+    out, grads = run(q, k, v, g, causal=causal, lengths=(lengths.cuda(), lengths.cuda()))
+    pick = [0, B - 1]
+    part = [t[pick][:, ::5].contiguous() for t in (q, k, v, g)]
+    peak = (g.float().norm(dim=-1).max() * v.float().norm(dim=-1).max()).item()
+    want = ref.attention(*part[:3], causal, ref.spans(2, n, n, lengths=(lengths[pick], lengths[pick])), do=part[3], peak=peak)
+    close(out[pick][:, ::5], want["out"], "out")
+    for name in grads:
+        close(grads[name][pick][:, ::5], want[name], name)
+
+
 def test_prepared_calls_and_refusals():
     from paper_2312_08874_amd import binding
     q, k, v, g = inputs("bf16", 2, 4, 2, 30, 50, 64)
