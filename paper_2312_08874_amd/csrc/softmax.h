@@ -72,10 +72,9 @@ constexpr int kSoftmaxUnits = 256;      // compute units
 
 // Whether blocks are of 64 rows and two waves share every 32 of them, each with half of every tile of 64 keys (or queries): where there are so
 // few blocks that the length of the longest is the time, and not so long ones that ranges are worth their parts.  `blocks`: of 64 rows,
-// `across`: what each goes over.  Measured, training steps, shared and not: 1500 tokens, 2 x 8
-// heads of 64, causal, 63 us and 88; 2 x 2000, 8 heads of 80 120 and 140; 4096, 8 heads of 64 187 and 214; but 8192 packed tokens, 8 heads, 1184
-// blocks, 108 and 100, and 2 x 1900, 16 heads of 128, 960 blocks, 427 and 355;
-// 2 x 4096, 16 heads on 4 of 128, whose keys are seen by 16384 rows, 919 and 648.
+// `across`: what each goes over.  Measured, training steps, shared and not: 1500 tokens, 2 x 8 heads of 64, causal, 63 us and 88; 2 x 2000,
+// 8 heads of 80 120 and 140; 4096, 8 heads of 64 187 and 214; but 8192 packed tokens, 8 heads, 1184 blocks, 108 and 100, 2 x 1900, 16 heads of
+// 128, 960 blocks, 427 and 355, and 2 x 4096, 16 heads on 4 of 128, whose keys 16384 rows see, 919 and 648.
 inline bool softmax_shared(int es, long long blocks, long long across) { return es == 2 && blocks < 3 * kSoftmaxUnits && across < 8192; }
 
 // Waves of a block of rows, 32 rows each: as few rounds of blocks over the compute units as may be, two waves where four would be half

@@ -266,6 +266,32 @@ def test_blocks_of_many_waves(dtype, d, causal):
         close(grads[name][pick][:, ::5], want[name], name)
 
 
+# dtype, B, Hq, Hk, queries, keys, d, causal, layout, mix
+EXTREMES = [
+    ("bf16", 1, 1, 1, 5, 7, 1, True, "dense", None),
+    ("f16", 2, 3, 1, 9, 40, 3, False, "odd", None),
+    ("f32", 1, 2, 1, 6, 33, 2, True, "token", None),
+    ("bf16", 1, 33, 1, 1, 200, 16, False, "token", None),
+    ("f16", 1, 64, 1, 2, 300, 64, True, "dense", None),
+    ("bf16", 1, 1, 1, 1, 70000, 64, False, "dense", None),
+    ("f32", 1, 5, 5, 2, 9000, 7, True, "dense", None),
+    ("f16", 1, 2, 1, 3000, 1, 32, False, "token", None),
+    ("bf16", 1, 2, 2, 1, 1, 256, True, "dense", None),
+    ("f16", 1, 7, 7, 65, 64, 255, True, "dense", None),
+    ("f32", 1, 1, 1, 33, 31, 129, False, "odd", None),
+    ("bf16", 1, 12, 1, 17, 17, 8, True, "qkv", ("packed", [17], [17])),
+    ("f16", 1, 2, 2, 4, 4, 16, False, "dense", ("packed", [0, 0, 0], [0, 0, 0])),
+    ("f32", 2, 2, 1, 4, 4, 16, False, "dense", ("padded", [0, 0], [0, 0])),
+]
+
+
+@pytest.mark.parametrize("case", EXTREMES, ids=[str(i) for i in range(len(EXTREMES))])
+def test_extremes(case):
+    """One channel and 256, one key and 70000, 64 heads on one, no sequence with a row."""
+    from tests.test_gpu_softmax import test_attention_and_its_gradients as check_case
+    check_case(case)
+
+
 def test_prepared_calls_and_refusals():
     from paper_2312_08874_amd import binding
     q, k, v, g = inputs("bf16", 2, 4, 2, 30, 50, 64)
