@@ -1007,14 +1007,18 @@ def _softmax_call(Q, K, V, causal, starts, lengths, scale):
     return desc, views
 
 
-def _fresh_tokens(t, zeros, stream):
-    """A result like t, in its order of axes where that is dense; zeros where rows of no sequence are left as they are."""
+def _fresh_tokens(like, zeros, stream):
+    """Results like these tensors, in their order of axes where that is dense; zeros where rows of no sequence are left as they are."""
     import torch
-    make = torch.zeros_like if zeros else torch.empty_like
-    if stream is None:
-        return make(t)
-    with torch.cuda.stream(stream):
-        return make(t)
+    if stream is not None:
+        with torch.cuda.stream(stream):
+            return _fresh_tokens(like, zeros, None)
+    # one launch clears all, 8 us of the host's time for three small tensors instead of 15, but 260 MB at 2.6 TB/s and not 4.7
+    together = zeros and sum(t.numel() for t in like) <= 1 << 20
+    results = [torch.empty_like(t) if together or not zeros else torch.zeros_like(t) for t in like]
+    if together:
+        torch._foreach_zero_(results)
+    return results
 
 
 def _softmax_workspace(need, workspace, stream, device):
@@ -1044,7 +1048,7 @@ def agent_softmax_attn_fwd(Q, K, V, *, causal=False, starts=None, lengths=None, 
     [S+1] on the device: S sequences packed into one batch element's rows.  scale 0: d^-1/2.  save: also returns what
     agent_softmax_attn_bwd needs, (out, saved).  Rows of no sequence: zeros, or what `out` held."""
     if out is None:
-        out = _fresh_tokens(Q, starts is not None or lengths is not None, stream)
+        out, = _fresh_tokens((Q,), starts is not None or lengths is not None, stream)
     args, saved, keep = _softmax_fwd_args(Q, K, V, causal, starts, lengths, scale, save, out, workspace, stream)
     _check(lib().agent_softmax_attn_fwd(*args), "agent_softmax_attn_fwd")
     return (out, saved) if save else out
@@ -1061,7 +1065,7 @@ def agent_softmax_attn_bwd(Q, K, V, out, saved, dO, *, causal=False, starts=None
         saved.numel() >= int(lib().agent_softmax_attn_saved_bytes(ctypes.byref(desc))), "saved is what the forward pass returned"
     o, g = _checked_view("out", out, Q, Q.shape), _checked_view("dO", dO, Q, Q.shape)
     if grads is None:
-        grads = tuple(_fresh_tokens(t, starts is not None or lengths is not None, stream) for t in (Q, K, V))
+        grads = _fresh_tokens((Q, K, V), starts is not None or lengths is not None, stream)
     dq, dk, dv = (_checked_view("d" + n, t, Q, like.shape) for n, t, like in zip("QKV", grads, (Q, K, V)))
     need = int(lib().agent_softmax_attn_bwd_workspace_bytes(ctypes.byref(desc), ctypes.byref(q), ctypes.byref(k), ctypes.byref(v),
                                                             ctypes.byref(g)))
