@@ -35,7 +35,7 @@ struct SoftmaxArgs {
   float scale, c;       // c = scale log2 e
   // columns kernel: query heads side by side in a tile, tokens of a tile, ranges of keys and where each leaves its part
   int pack, tile_tokens, splits;
-  float *part, *part_ml;      // [split][batch, head, token][d], [..][2]
+  float *part, *part_stats;      // [split][batch, head, token][d]; [..][3]: reference, sum, what rounding took from it
   // backward pass: what the queries' kernel leaves for the keys' of every query, [2][batch][heads_q][tokens_q], and fp16's peaks
   float* stats;
   float* peaks;         // [2][kPeakBlocks]: of each of peak_blocks blocks, the largest squared length of a row of dout, and of v

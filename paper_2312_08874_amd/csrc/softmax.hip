@@ -185,7 +185,7 @@ size_t softmax_fwd_workspace(int dtype, const SoftmaxArgs& a) {
   const int terms = p.columns ? 1 : softmax_terms(es, softmax_width(a.d));
   size_t bytes = copy_bytes(a.q, a.batch, a.heads_q, a.tokens_q, a.d, es, terms) + copy_bytes(a.k, a.batch, a.heads_k, a.tokens_k, a.d, es, terms) +
                  copy_bytes(a.v, a.batch, a.heads_k, a.tokens_k, a.d, es, terms);
-  if (p.splits > 1) bytes += aligned((size_t)p.splits * query_rows(a) * a.d * 4) + aligned((size_t)p.splits * query_rows(a) * 8);
+  if (p.splits > 1) bytes += aligned((size_t)p.splits * query_rows(a) * a.d * 4) + aligned((size_t)p.splits * query_rows(a) * 12);
   return bytes;
 }
 
@@ -200,7 +200,7 @@ hipError_t launch_softmax_fwd(int dtype, SoftmaxArgs a, void* workspace, hipStre
   a.waves = p.waves, a.shared = p.shared, a.pack = p.pack, a.tile_tokens = p.tile_tokens, a.splits = p.splits;
   if (p.splits > 1) {
     a.part = (float*)ws;
-    a.part_ml = (float*)(ws + aligned((size_t)p.splits * query_rows(a) * a.d * 4));
+    a.part_stats = (float*)(ws + aligned((size_t)p.splits * query_rows(a) * a.d * 4));
   }
   err = launch(dtype, a, p.columns ? SoftmaxPass::kColumns : SoftmaxPass::kRows, p.tiles, st);
   return err != hipSuccess || p.splits == 1 ? err : launch(dtype, a, SoftmaxPass::kJoin, 0, st);
