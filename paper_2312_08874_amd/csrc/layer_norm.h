@@ -1,5 +1,5 @@
-// Layer norm: what the C-ABI layer hands to the kernels, and the rule that shares a row out among lanes.  Plain C++ with no GPU
-// dependency, so that the rule can be tested without a GPU.
+// Layer norm: what the C-ABI layer hands to the kernels, and the rule that shares a row out among lanes.  Plain C++ but for
+// float2, so that the rule can be tested without a GPU.
 #pragma once
 #include <stddef.h>
 #include <stdint.h>
@@ -43,6 +43,13 @@ inline NormShape norm_shape(int es, int width, bool backward) {
     while (s.lanes > 1 && s.lanes / 2 * 2 >= count) s.lanes /= 2;      // two pieces a lane where rows are short
   while (s.lanes * s.pieces < count) s.pieces *= 2;
   return s;
+}
+
+// What norm_shape comes to, and so what the kernels are compiled for: rows shared by blocks of `threads`, or (block false) by up to a wave.
+constexpr bool norm_takes(int es, int threads, bool block, int pieces, bool backward) {
+  const int most = (backward ? 16 : 32) * es / 16;
+  if (!block) return pieces <= most;
+  return pieces >= most / 2 && pieces <= (backward && threads == 1024 ? 2 * most : most);
 }
 
 // Blocks of the backward pass, each of which leaves a part of the weights' gradients, two for each compute unit: training steps of
