@@ -447,8 +447,9 @@ size_t agent_softmax_attn_workspace_bytes(const aa_softmax_attn *desc, const aa_
 size_t agent_softmax_attn_bwd_workspace_bytes(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,
                                               const aa_view *dout);
 /* saved: NULL, or agent_softmax_attn_saved_bytes() of device memory, 256-byte aligned, for the backward pass: lse, fp32,
- * [batch][heads_q][tokens_q], from the start on, and for 16-bit types what rounding took from out, which D below is off without where
- * rows see few keys (its gradients by twice their rounding).  Results overlap nothing (slices of one buffer as above).
+ * [batch][heads_q][tokens_q], from the start on, and for 16-bit types, unless whole sequences of more than 512 keys are seen by every row,
+ * what rounding took from out, which D below is off without where rows see few keys (its gradients by twice their rounding).
+ * Results overlap nothing (slices of one buffer as above).
  * Errors: AA_ERR_NULL, AA_ERR_SHAPE, AA_ERR_DTYPE, AA_ERR_UNSUPPORTED (d > 256, more blocks or elements than can be numbered),
  * AA_ERR_WORKSPACE (256-byte aligned), AA_ERR_ALIAS. */
 aa_status agent_softmax_attn_fwd(const aa_softmax_attn *desc, const aa_view *q, const aa_view *k, const aa_view *v,

@@ -83,7 +83,7 @@ bool any_meet(const TokenSpan (&results)[R], const TokenSpan (&inputs)[I], const
 // what the forward pass keeps: its place
 void keep(const aa_softmax_attn* d, const void* saved, SoftmaxArgs* a) {
   a->lse = (float*)const_cast<void*>(saved);
-  a->low = saved && d->dtype != AA_F32 ? (char*)const_cast<void*>(saved) + aa::softmax_saved_lse(*a) : nullptr;
+  a->low = saved && aa::softmax_keeps_low(d->dtype, *a) ? (char*)const_cast<void*>(saved) + aa::softmax_saved_lse(*a) : nullptr;
 }
 
 }  // namespace

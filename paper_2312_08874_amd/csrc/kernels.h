@@ -145,8 +145,9 @@ hipError_t launch_softmax_bwd_f16(const SoftmaxArgs& a, SoftmaxPass pass, int ti
 hipError_t launch_softmax_bwd_bf16(const SoftmaxArgs& a, SoftmaxPass pass, int tiles, hipStream_t st);
 // whether the blocks of these sizes can be numbered
 bool softmax_fits(int dtype, const SoftmaxArgs& a);
-// what the forward pass keeps: lse from the start on, behind its bytes what rounding took from out (16-bit types)
+// what the forward pass keeps: lse from the start on, behind its bytes what rounding took from out (16-bit types, where rows may see few keys)
 size_t softmax_saved_lse(const SoftmaxArgs& a);
+bool softmax_keeps_low(int dtype, const SoftmaxArgs& a);
 size_t softmax_saved_bytes(int dtype, const SoftmaxArgs& a);
 // workspaces (tensors without an address: of any alignment), launches
 size_t softmax_fwd_workspace(int dtype, const SoftmaxArgs& a);

@@ -175,8 +175,12 @@ bool softmax_fits(int dtype, const SoftmaxArgs& a) {      // blocks are numbered
 }
 
 size_t softmax_saved_lse(const SoftmaxArgs& a) { return aligned((size_t)query_rows(a) * 4); }
+bool softmax_keeps_low(int dtype, const SoftmaxArgs& a) {
+  const bool all_long = a.sequences == 0 && !a.causal && a.lengths_k == nullptr && a.tokens_k > kLowKeys;      // no row sees so few keys
+  return dtype != 0 && !all_long;
+}
 size_t softmax_saved_bytes(int dtype, const SoftmaxArgs& a) {
-  return softmax_saved_lse(a) + (dtype == 0 ? 0 : aligned((size_t)query_rows(a) * a.d * 2));
+  return softmax_saved_lse(a) + (softmax_keeps_low(dtype, a) ? aligned((size_t)query_rows(a) * a.d * 2) : 0);
 }
 
 size_t softmax_fwd_workspace(int dtype, const SoftmaxArgs& a) {
