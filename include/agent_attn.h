@@ -425,8 +425,9 @@ aa_status agent_gated_ffn_bwd(const aa_ffn *desc, const void *x, const aa_ffn_we
  * Rows of no sequence are not used, whatever they hold, and as results stay as they were.  Lengths and starts are read on the
  * device and kept within the tensors' rows there; starts that fall give results of no meaning.
  * Scores and sums are fp32; p (and, backward, ds) is rounded to dtype, as an operand (fp32: products are taken of three bf16
- * terms of either operand, to 2^-24 of the largest, up to d 128 and for more than few queries); results are rounded once.  fp16: ds is held
- * in steps of 2^-37 of the product of the call's longest rows of dout and v, which much smaller gradients beside it lose digits to.
+ * terms of either operand, to 2^-24 of the largest, up to d 128 and for more than few queries); results are rounded once.  fp16: p is held
+ * to 2^-31 of the row's largest, ds in steps of 2^-37 of the product of the call's longest rows of dout and v, which much smaller gradients beside
+ * it lose digits to.
  * A NaN or infinity in a row of a sequence may show in every result of that head's sequence.  d <= 256. */
 typedef struct {
   int32_t batch, heads_q, heads_k; /* heads_q a multiple of heads_k */

@@ -33,7 +33,10 @@ struct NormShape {
   int rows_at_once() const { return lanes >= threads ? 1 : threads / lanes; }
 };
 // At most 32 channels a lane forward and, where rows are no longer than a block of 1024 takes so, 16 backward, whose lanes also hold the next
-// row and the sums of the weights' gradients.
+// row and the sums of the weights' gradients.  Backward, blocks of 1024 have 128 registers a lane, which is too few above 8192 channels: up to 16384
+// 64 to 146 are spilled in 16 bits and up to 203 in fp32, above that 528 to 711 and up to 1022.  A step of 4096 rows in bf16, both ways with the
+// residual, takes 166 us of 8192 channels, 384 of 16384 and 1677 of 32768, where a large copy's rate gives 98, 196 and 392; in fp32 258, 1004 and 3418
+// (196, 392 and 785).
 inline NormShape norm_shape(int es, int width, bool backward) {
   const int per = 16 / es, count = (width + per - 1) / per, most = (backward && width <= 16384 ? 16 : 32) / per;
   NormShape s{64, 1, 256};
@@ -52,8 +55,8 @@ constexpr bool norm_takes(int es, int threads, bool block, int pieces, bool back
   return pieces >= most / 2 && pieces <= (backward && threads == 1024 ? 2 * most : most);
 }
 
-// Blocks of the backward pass, each of which leaves a part of the weights' gradients, two for each compute unit: training steps of
-// 65536 x 2048 in fp16 take 429 us (256 blocks: 554, 768: 438), of 16384 x 512 in bf16 37 (any of these).
+// Blocks of the backward pass, each of which leaves a part of the weights' gradients, two for each compute unit: training steps with the residual
+// of 65536 x 2048 in fp16 take 478 us (256 blocks: 573, 768: 493), in fp32 930 (946, 967), of 16384 x 512 in bf16 37 (any of these).
 constexpr int kNormBlocks = 512;
 inline int norm_blocks(const NormShape& s, int rows, bool backward) {
   const long long needed = ((long long)rows + s.rows_at_once() - 1) / s.rows_at_once();
